@@ -323,6 +323,107 @@ rl_da_status rl_kv_append(const void* k_new, const void* v_new, void* k_pool, vo
                           int32_t layout, int32_t* device_error, void* stream);
 
 /*
+ * Rotate and append: rl_kv_append for new tokens as the projections leave them.
+ * Each query and key head row x of a token is normalised (optional), rotated by
+ * the token's position and rounded once; keys and values join the cache, queries
+ * go to q_out, which the attention of the same step reads (rl_decode_attn_run and
+ * rl_prefix_attn for one token per sequence, rl_extend_attn for several):
+ *     x <- x / sqrt(mean(x^2) + norm_eps) * w       (w: q_norm or k_norm)
+ *     (a, b) <- (a c - b s, b c + a s)              for each pair of x
+ * Values are appended as they are.
+ *   q, k_new, v_new  bf16, head rows [num_q_heads or num_kv_heads][head_dim]
+ *                contiguous within a token, tokens q_stride, k_stride, v_stride
+ *                elements apart (multiples of 8), so that the three may be views
+ *                of one projection's output
+ *   q_start      [batch + 1] int32, non-decreasing from 0: sequence b's new tokens
+ *                are rows q_start[b] .. q_start[b + 1] - 1, none or several;
+ *                max_q_per_seq >= their number (sizes the grid).  NULL: one token
+ *                per sequence, row b (max_q_per_seq 1)
+ *   seq_lens     [batch] int32, each sequence's length BEFORE the append: its new
+ *                token i has position seq_lens[b] + i and goes to page
+ *                block_table[b][position / page_size], slot position % page_size
+ *   cos_sin      [num_positions][rotary_dim] fp32: a position's rotary_dim / 2
+ *                cosines, then its sines (the caller's own frequencies and scaling)
+ *   interleaved  0: pair i is dims i and i + rotary_dim / 2;  else dims 2i, 2i + 1.
+ *                Dims from rotary_dim on are not rotated
+ *   q_norm, k_norm  [head_dim] bf16 weights, both or neither
+ *   q_out        [T][num_q_heads][head_dim] bf16, T = q_start[batch] (batch); may be
+ *                q itself if q_stride is num_q_heads * head_dim
+ * bf16 pools: the row rounded to bf16.  e4m3 pools: as rl_kv_append, with all new
+ * tokens of a (page, kv head) slab joining at once: scale' = max over the earlier
+ * scale (if the slab holds earlier tokens of the sequence) and the new tokens'
+ * absmax / 448, earlier codes re-encoded when it grows, new rows encoded from
+ * fp32.  For values, and keys that no rotation changes, one token at a time
+ * gives rl_kv_append's bytes.
+ *
+ * As for rl_kv_append, different sequences must append into different slabs; a
+ * sequence with seq_lens[b] < 0 is skipped, and so, reported in device_error when
+ * that is non-NULL, are tokens at positions from max_pages * page_size or from
+ * num_positions on (RL_DA_DEVERR_LENGTH_TOO_LONG) and tokens whose page is outside
+ * [0, num_pages) (RL_DA_DEVERR_PAGE_OUT_OF_RANGE): nothing of a skipped token is
+ * written, its row of q_out included.  Needs no handle and no workspace; enqueues
+ * one kernel on `stream`.  Any rl_da_layout; head_dim 128, page_size 16, rotary_dim
+ * a multiple of 16 up to 128 only (else UNSUPPORTED); q, k_new, v_new, cos_sin, the
+ * norm weights, q_out and the pools 16-byte aligned.
+ */
+rl_da_status rl_rope_append(const void* q, int64_t q_stride, const void* k_new, int64_t k_stride,
+                            const void* v_new, int64_t v_stride, const int32_t* q_start,
+                            int32_t max_q_per_seq, const float* cos_sin, int32_t num_positions,
+                            int32_t rotary_dim, int32_t interleaved, const void* q_norm,
+                            const void* k_norm, float norm_eps, void* q_out, void* k_pool,
+                            void* v_pool, float* k_scale, float* v_scale, int64_t num_pages,
+                            const int32_t* block_table, int32_t max_pages,
+                            const int32_t* seq_lens, int32_t batch, int32_t num_q_heads,
+                            int32_t num_kv_heads, int32_t head_dim, int32_t page_size,
+                            int32_t kv_dtype, int32_t layout, int32_t* device_error,
+                            void* stream);
+
+/*
+ * Decode attention over shared prefixes: rl_decode_attn_run's result for a batch
+ * whose sequences share their first pages in groups (the responses to one prompt,
+ * 8 of each in the paper's rollouts, Sec. 7.1; a system prompt under all of them),
+ * with each group's shared pages read once instead of once per sequence.
+ *   group_start   [num_groups + 1] int32, non-decreasing: group g is sequences
+ *                 group_start[g] .. group_start[g + 1] - 1; sequences before the first
+ *                 group and behind the last share nothing
+ *   prefix_pages  [num_groups] int32: that many leading entries of the block-table
+ *                 rows are the same in all of the group's members (clamped to
+ *                 0 .. max_pages)
+ * A sequence of fewer than prefix_pages * page_size tokens is no member of its
+ * group: it attends its own row, and may hold anything there if it is empty.  q,
+ * pools, scales, block_table, seq_lens and out as for rl_decode_attn_run;
+ * num_groups 0 (group_start and prefix_pages then unread) is a plain decode step.
+ *
+ * The workspace is device memory of at least rl_prefix_attn_workspace_size bytes
+ * for these sizes, 16-byte aligned; the launches of this call alone write and read
+ * it, so it needs no initial contents, may be reused or freed once the stream has
+ * passed them, and calls that can overlap bring one each.  Enqueues three kernels on
+ * `stream` and allocates nothing.  Deterministic: keys are cut where the call's sizes
+ * and the sequence's and its prefix's lengths say, and a row's partial results join
+ * in a fixed order.
+ *
+ * Block-table entries are checked on the device: one outside [0, num_pages) among a
+ * sequence's (a group's shared) pages is reported in device_error, when that is
+ * non-NULL, with RL_DA_DEVERR_PAGE_OUT_OF_RANGE, and the outputs of that sequence
+ * (that group's members) are then undefined; a length beyond max_pages * page_size
+ * is cut there and reported with RL_DA_DEVERR_LENGTH_TOO_LONG.  The bits are only
+ * ever set.  head_dim 128, page_size 16, Hq / Hkv in {1, 2, 4, 8, 16} (else
+ * UNSUPPORTED); q, the pools and out 16-byte aligned.
+ */
+rl_da_status rl_prefix_attn_workspace_size(int32_t max_pages, int32_t batch, int32_t num_groups,
+                                           int32_t num_q_heads, int32_t num_kv_heads,
+                                           size_t* bytes);
+rl_da_status rl_prefix_attn(const void* q, const void* k_pool, const void* v_pool,
+                            const float* k_scale, const float* v_scale, int64_t num_pages,
+                            const int32_t* block_table, int32_t max_pages,
+                            const int32_t* seq_lens, int32_t batch, const int32_t* group_start,
+                            const int32_t* prefix_pages, int32_t num_groups, int32_t num_q_heads,
+                            int32_t num_kv_heads, int32_t head_dim, int32_t page_size,
+                            int32_t kv_dtype, int32_t layout, float scale, void* out,
+                            void* workspace, size_t workspace_bytes, int32_t* device_error,
+                            void* stream);
+
+/*
  * Measurement hook (no counterpart in the paper): with both events non-NULL,
  * every later run() launches its split-K kernel with split_begin and
  * split_end attached to the launch itself (hipExtLaunchKernel), so they take

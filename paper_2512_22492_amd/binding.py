@@ -52,6 +52,9 @@ EXPORTED = [
     "rl_extend_attn_workspace_size",
     "rl_extend_attn_ws",
     "rl_kv_append",
+    "rl_rope_append",
+    "rl_prefix_attn_workspace_size",
+    "rl_prefix_attn",
     "rl_decode_attn_set_timing_events",
     "rl_ws_plan",
     "rl_ws_create",
@@ -156,6 +159,16 @@ def load_library():
     lib.rl_kv_append.argtypes = [vp, vp, vp, vp, vp, vp, i64, vp, i32, vp, i32, i32, i32, i32,
                                  i32, i32, vp, vp]
     lib.rl_kv_append.restype = ctypes.c_int
+    lib.rl_rope_append.argtypes = ([vp, i64, vp, i64, vp, i64, vp, i32, vp, i32, i32, i32, vp, vp,
+                                    ctypes.c_float, vp, vp, vp, vp, vp, i64, vp, i32, vp]
+                                   + [i32] * 7 + [vp, vp])
+    lib.rl_rope_append.restype = ctypes.c_int
+    lib.rl_prefix_attn_workspace_size.argtypes = [i32] * 5 + [ctypes.POINTER(ctypes.c_size_t)]
+    lib.rl_prefix_attn_workspace_size.restype = ctypes.c_int
+    lib.rl_prefix_attn.argtypes = [vp, vp, vp, vp, vp, i64, vp, i32, vp, i32, vp, vp, i32, i32,
+                                   i32, i32, i32, i32, i32, ctypes.c_float, vp, vp,
+                                   ctypes.c_size_t, vp, vp]
+    lib.rl_prefix_attn.restype = ctypes.c_int
     lib.rl_decode_attn_set_timing_events.argtypes = [vp, vp, vp]
     lib.rl_decode_attn_set_timing_events.restype = ctypes.c_int
     u64 = ctypes.c_uint64
@@ -466,6 +479,247 @@ def kv_append(p, k_new, v_new, device_error=None, stream=None):
     """Appends k_new/v_new [B, Hkv, D] (bf16 tensors) to problem p's pools at
     positions p.seq_lens; raises on a bad status."""
     KvAppender(p, device_error)(k_new, v_new, stream)
+
+
+def rl_rope_append(q, q_stride, k_new, k_stride, v_new, v_stride, q_start, max_q_per_seq,
+                   cos_sin, num_positions, rotary_dim, interleaved, q_norm, k_norm, norm_eps,
+                   q_out, k_pool, v_pool, k_scale, v_scale, num_pages, block_table, max_pages,
+                   seq_lens, batch, num_q_heads, num_kv_heads, head_dim=128, page_size=16,
+                   kv_dtype=RL_DA_KV_BF16, layout=RL_DA_LAYOUT_HND, device_error=None,
+                   stream=None) -> int:
+    return load_library().rl_rope_append(
+        _ptr(q), int(q_stride), _ptr(k_new), int(k_stride), _ptr(v_new), int(v_stride),
+        _ptr(q_start), int(max_q_per_seq), _ptr(cos_sin), int(num_positions), int(rotary_dim),
+        int(interleaved), _ptr(q_norm), _ptr(k_norm), float(norm_eps), _ptr(q_out),
+        _ptr(k_pool), _ptr(v_pool), _ptr(k_scale), _ptr(v_scale), int(num_pages),
+        _ptr(block_table), int(max_pages), _ptr(seq_lens), int(batch), int(num_q_heads),
+        int(num_kv_heads), int(head_dim), int(page_size), int(kv_dtype), int(layout),
+        _ptr(device_error), _stream(stream))
+
+
+def _device_index(device):
+    """The index of the GPU that an object's launches go to; raises ValueError for
+    tensors that are not on one."""
+    import torch
+    if device.type != "cuda":
+        raise ValueError("the cache is on %s, expected a GPU" % device)
+    return torch.cuda.current_device() if device.index is None else device.index
+
+
+def _on_device(index, call):
+    """call() with the GPU `index` current, where the library launches."""
+    import torch
+    if torch.cuda.current_device() == index:
+        return call()
+    with torch.cuda.device(index):
+        return call()
+
+
+def _token_stride(name, t, heads, head_dim, dtype, device, tokens=None):
+    """The token stride of head rows [T, heads, head_dim] that are contiguous within a
+    token (a slice of a fused projection's heads, say); raises ValueError else."""
+    _check_tensor(name, t, dtype=dtype, shape=(tokens, heads, head_dim), device=device,
+                  contiguous=False)
+    if t.numel() == 0 or t.is_contiguous():
+        return heads * head_dim
+    stride, row, one = t.stride()
+    if one != 1 or (heads > 1 and row != head_dim):
+        raise ValueError("%s must have contiguous head rows, has strides %s" % (name, t.stride()))
+    if t.shape[0] == 1:
+        return heads * head_dim
+    if stride < heads * head_dim or stride % 8:
+        raise ValueError("%s must have a token stride that is a multiple of 8 and holds its "
+                         "heads, has %d" % (name, stride))
+    return stride
+
+
+class RopeAppender:
+    """rl_rope_append for a loop that appends to one cache step after step: checks
+    problem p's cache tensors, the rotation table cos_sin [positions, rotary_dim] fp32
+    (cosines, then sines) and the norm weights once, here, and only the new tokens
+    on each call.  They must keep their storage, dtype and shape while the appender
+    is used (their contents may change)."""
+
+    def __init__(self, p, cos_sin, *, q_norm=None, k_norm=None, eps=1e-6, interleaved=False,
+                 device_error=None):
+        import torch
+        dt = RL_DA_KV_BF16 if p.kv_dtype == "bf16" else RL_DA_KV_FP8_E4M3
+        dev = self.device = p.k_pool.device
+        self.batch, self.head_dim = p.batch, p.head_dim
+        self.num_q_heads, self.num_kv_heads = p.num_q_heads, p.num_kv_heads
+        _check_pools(p.k_pool, p.v_pool, p.k_scale, p.v_scale, kv_dtype=dt,
+                     layout=LAYOUTS[p.layout], num_kv_heads=p.num_kv_heads,
+                     head_dim=p.head_dim, page_size=p.page_size, device=dev)
+        _check_table(p.block_table, p.seq_lens, p.batch, dev)
+        _check_tensor("cos_sin", cos_sin, dtype=torch.float32, ndim=2, device=dev)
+        if (q_norm is None) != (k_norm is None):
+            raise ValueError("q_norm and k_norm come together or not at all")
+        for name, w in (("q_norm", q_norm), ("k_norm", k_norm)):
+            if w is not None:
+                _check_tensor(name, w, dtype=torch.bfloat16, shape=(p.head_dim,), device=dev)
+        if device_error is not None:
+            _check_tensor("device_error", device_error, dtype=torch.int32, device=dev)
+        # what the addresses below belong to
+        self._held = (p.k_pool, p.v_pool, p.k_scale, p.v_scale, p.block_table, p.seq_lens,
+                      cos_sin, q_norm, k_norm, device_error)
+        self._fn = load_library().rl_rope_append
+        self._turn_args = (_ptr(cos_sin), int(cos_sin.shape[0]), int(cos_sin.shape[1]),
+                           int(bool(interleaved)), _ptr(q_norm), _ptr(k_norm), float(eps))
+        self._cache_args = (
+            _ptr(p.k_pool), _ptr(p.v_pool), _ptr(p.k_scale), _ptr(p.v_scale), int(p.num_pages),
+            _ptr(p.block_table), int(p.max_pages), _ptr(p.seq_lens), int(p.batch),
+            int(p.num_q_heads), int(p.num_kv_heads), int(p.head_dim), int(p.page_size), dt,
+            LAYOUTS[p.layout], _ptr(device_error))
+        self._index = _device_index(dev)
+
+    def __call__(self, q, k_new, v_new, q_out, q_start=None, max_q_per_seq=1, stream=None):
+        """Rotates q [T, Hq, D] into q_out (which may be q) and appends k_new, rotated,
+        and v_new [T, Hkv, D] (bf16) from positions seq_lens on: one token per sequence,
+        or with q_start [B + 1] rows q_start[b] .. q_start[b + 1] - 1 of sequence b, at
+        most max_q_per_seq of them; raises on a bad status."""
+        import torch
+        dev, bf16, D = self.device, torch.bfloat16, self.head_dim
+        tokens = self.batch if q_start is None else None
+        if q_start is not None:
+            _check_tensor("q_start", q_start, dtype=torch.int32, shape=(self.batch + 1,),
+                          device=dev)
+            tokens = int(q.shape[0]) if hasattr(q, "shape") and len(q.shape) else None
+        qs = _token_stride("q", q, self.num_q_heads, D, bf16, dev, tokens)
+        ks = _token_stride("k_new", k_new, self.num_kv_heads, D, bf16, dev, tokens)
+        vs = _token_stride("v_new", v_new, self.num_kv_heads, D, bf16, dev, tokens)
+        _check_tensor("q_out", q_out, dtype=bf16, shape=(tokens, self.num_q_heads, D),
+                      device=dev)
+        if tokens == 0:
+            return
+        rc = _on_device(self._index, lambda: self._fn(
+            q.data_ptr(), qs, k_new.data_ptr(), ks, v_new.data_ptr(), vs, _ptr(q_start),
+            int(max_q_per_seq), *self._turn_args, q_out.data_ptr(), *self._cache_args,
+            _stream(stream)))
+        if rc != RL_DA_OK:
+            raise RLDecodeAttnError(rc, "rl_rope_append")
+
+
+def rope_append(p, q, k_new, v_new, cos_sin, q_out, q_start=None, max_q_per_seq=1, stream=None,
+                **kw):
+    """One RopeAppender call on problem p's cache (keywords as RopeAppender's)."""
+    RopeAppender(p, cos_sin, **kw)(q, k_new, v_new, q_out, q_start, max_q_per_seq, stream)
+
+
+def rl_prefix_attn_workspace_size(max_pages, batch, num_groups, num_q_heads, num_kv_heads):
+    """Returns (status, bytes)."""
+    n = ctypes.c_size_t()
+    rc = load_library().rl_prefix_attn_workspace_size(
+        int(max_pages), int(batch), int(num_groups), int(num_q_heads), int(num_kv_heads),
+        ctypes.byref(n))
+    return rc, n.value
+
+
+def rl_prefix_attn(q, k_pool, v_pool, k_scale, v_scale, num_pages, block_table, max_pages,
+                   seq_lens, batch, group_start, prefix_pages, num_groups, num_q_heads,
+                   num_kv_heads, head_dim=128, page_size=16, kv_dtype=RL_DA_KV_BF16,
+                   layout=RL_DA_LAYOUT_HND, scale=1.0, out=None, workspace=None,
+                   workspace_bytes=0, device_error=None, stream=None) -> int:
+    return load_library().rl_prefix_attn(
+        _ptr(q), _ptr(k_pool), _ptr(v_pool), _ptr(k_scale), _ptr(v_scale), int(num_pages),
+        _ptr(block_table), int(max_pages), _ptr(seq_lens), int(batch), _ptr(group_start),
+        _ptr(prefix_pages), int(num_groups), int(num_q_heads), int(num_kv_heads),
+        int(head_dim), int(page_size), int(kv_dtype), int(layout), float(scale), _ptr(out),
+        _ptr(workspace), int(workspace_bytes), _ptr(device_error), _stream(stream))
+
+
+class PrefixAttention:
+    """rl_prefix_attn for a loop that decodes over one cache step after step: checks
+    problem p's cache tensors and the groups once, here, and only q and out on each
+    call.  group_start [groups + 1] and prefix_pages [groups] are int32 tensors on the
+    pools' device; like the cache tensors they must keep their storage, dtype and
+    shape while the object is used (their contents may change).
+
+    workspace: a contiguous uint8 tensor of at least rl_prefix_attn_workspace_size
+    bytes for these sizes, by default one of the object's own.  One launch uses it at
+    a time: streams, and captured graphs that can overlap, bring one each."""
+
+    def __init__(self, p, group_start, prefix_pages, workspace=None, device_error=None):
+        import torch
+        dt = RL_DA_KV_BF16 if p.kv_dtype == "bf16" else RL_DA_KV_FP8_E4M3
+        dev = self.device = p.k_pool.device
+        self.want = (p.batch, p.num_q_heads, p.head_dim)
+        _check_pools(p.k_pool, p.v_pool, p.k_scale, p.v_scale, kv_dtype=dt,
+                     layout=LAYOUTS[p.layout], num_kv_heads=p.num_kv_heads,
+                     head_dim=p.head_dim, page_size=p.page_size, device=dev)
+        _check_table(p.block_table, p.seq_lens, p.batch, dev)
+        _check_tensor("prefix_pages", prefix_pages, dtype=torch.int32, ndim=1, device=dev)
+        groups = int(prefix_pages.shape[0])
+        _check_tensor("group_start", group_start, dtype=torch.int32, shape=(groups + 1,),
+                      device=dev)
+        if device_error is not None:
+            _check_tensor("device_error", device_error, dtype=torch.int32, device=dev)
+        rc, need = rl_prefix_attn_workspace_size(p.max_pages, p.batch, groups, p.num_q_heads,
+                                                 p.num_kv_heads)
+        if rc != RL_DA_OK:
+            raise RLDecodeAttnError(rc, "rl_prefix_attn_workspace_size")
+        self._index = _device_index(dev)
+        self._streams = None
+        if workspace is None:
+            workspace = self._own_workspace(need)
+        _check_tensor("workspace", workspace, dtype=torch.uint8, ndim=1, device=dev)
+        if int(workspace.shape[0]) < need:
+            raise ValueError("workspace has %d bytes, needs %d" % (workspace.shape[0], need))
+        self.workspace = workspace
+        # what the addresses below belong to
+        self._held = (p.k_pool, p.v_pool, p.k_scale, p.v_scale, p.block_table, p.seq_lens,
+                      group_start, prefix_pages, device_error)
+        self._fn = load_library().rl_prefix_attn
+        self._before = (_ptr(p.k_pool), _ptr(p.v_pool), _ptr(p.k_scale), _ptr(p.v_scale),
+                        int(p.num_pages), _ptr(p.block_table), int(p.max_pages),
+                        _ptr(p.seq_lens), int(p.batch), _ptr(group_start), _ptr(prefix_pages),
+                        groups, int(p.num_q_heads), int(p.num_kv_heads), int(p.head_dim),
+                        int(p.page_size), dt, LAYOUTS[p.layout], float(p.scale))
+        self._behind = (_ptr(workspace), int(workspace.shape[0]), _ptr(device_error))
+
+    def _own_workspace(self, nbytes):
+        """Memory that any stream may use at once: the allocator hands out memory whose
+        last user on the current stream may still run, so that is waited for (not
+        under graph capture, whose memory is the graph's own)."""
+        import torch
+        with torch.cuda.device(self._index):
+            ws = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+            now = torch.cuda.current_stream()
+            self._streams = {now.cuda_stream}
+            if not torch.cuda.is_current_stream_capturing() and not now.query():
+                now.synchronize()
+        return ws
+
+    def _note_stream(self, stream):
+        """Keeps the object's own workspace from being handed on, once the object is
+        gone, before its launches on `stream` have ended."""
+        import torch
+        handle = _stream(stream) or 0
+        if handle not in self._streams:
+            self._streams.add(handle)
+            if handle == 0:
+                s = torch.cuda.default_stream(self._index)
+            else:
+                s = torch.cuda.ExternalStream(handle, device=self.device)
+            self.workspace.record_stream(s)
+
+    def __call__(self, q, out, stream=None):
+        """One decode step of q [B, Hq, D] into out; raises on a bad status."""
+        import torch
+        _check_tensor("q", q, dtype=torch.bfloat16, shape=self.want, device=self.device)
+        _check_tensor("out", out, dtype=torch.bfloat16, shape=self.want, device=self.device)
+        if self._streams is not None:
+            self._note_stream(stream)
+        rc = _on_device(self._index, lambda: self._fn(
+            q.data_ptr(), *self._before, out.data_ptr(), *self._behind, _stream(stream)))
+        if rc != RL_DA_OK:
+            raise RLDecodeAttnError(rc, "rl_prefix_attn")
+
+
+def prefix_attention(p, group_start, prefix_pages, out, stream=None, workspace=None,
+                     device_error=None):
+    """One decode step of problem p (its q) whose groups of sequences share their first
+    pages, as PrefixAttention; raises on a bad status."""
+    PrefixAttention(p, group_start, prefix_pages, workspace, device_error)(p.q, out, stream)
 
 
 def rl_decode_attn_set_timing_events(h, split_begin, split_end) -> int:

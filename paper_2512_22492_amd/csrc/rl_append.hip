@@ -1,6 +1,6 @@
 // rl_append.hip -- KV-cache append (bf16 copy, e4m3 with growing slab scales).
 
-#include "rl_common.h"
+#include "rl_e4m3.h"
 
 using namespace rl_da;
 
@@ -35,18 +35,6 @@ __device__ __forceinline__ float wave_max(float v)
     v = fmaxf(v, __shfl_xor(v, 16));
     v = fmaxf(v, __shfl_xor(v, 32));
     return v;
-}
-
-// Two fp32 values to two e4m3 codes (round to nearest even) in the low 16 bits.
-__device__ __forceinline__ uint32_t e4m3_pair(float a, float b)
-{
-    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false) & 0xffffu;
-}
-
-__device__ __forceinline__ float clamp448(float v)
-{
-    // comparisons, not fminf/fmaxf, so that a NaN passes through unchanged
-    return v > 448.0f ? 448.0f : (v < -448.0f ? -448.0f : v);
 }
 
 template <bool FP8>
