@@ -31,7 +31,7 @@ namespace {
 constexpr int kMaxSplitPages = kWave * kUnitWaves;  // a lane of each wavefront per page
 constexpr int kMinSplitPages = 16;
 constexpr int kTargetUnits = 1024;
-constexpr int kTileRows = 16;
+constexpr int kTileRows = 128;        // query rows of a shared unit at most
 constexpr float kNoScore = -3.0e38f;  // running max before the first key
 
 // Splits of a run of `pages` pages: no longer than kMaxSplitPages, and for runs of
@@ -66,6 +66,11 @@ struct Unit {
     int32_t need;   // rows of sequences shorter than this are left out
 };
 
+struct Queue {
+    int32_t units;  // of the plan, each for num_kv_heads kv heads
+    int32_t next;   // first one that no work-group has taken
+};
+
 struct PrefixArgs {
     const uint16_t* q;          // bf16 [B][Hq][D]
     const uint8_t* k_pool;
@@ -78,7 +83,8 @@ struct PrefixArgs {
     const int32_t* prefix_pages;
     uint16_t* out;              // bf16 [B][Hq][D]
     int32_t* dev_error;         // may be null
-    int32_t* num_units;         // workspace
+    Queue* queue;               // workspace
+    int32_t* leaders;           // workspace [num_groups]
     int2* parts;                // workspace [B]: shared and own partial results
     Unit* units;                // workspace
     float2* ml;                 // workspace [B * Hq][slots]: max (log2 units), weight sum
@@ -97,15 +103,17 @@ struct PrefixArgs {
     int32_t slots;
     int32_t wanted_shared;      // splits that fill the device (splits_of)
     int32_t wanted_own;
-    float scale_log2;           // scale * log2(e)
+    float scale_log2;           // |scale| * log2(e)
+    uint32_t q_sign;            // 0x80008000 for a negative scale: Q enters negated
 };
 
 // ------------------------------------------------------------------ plan ---
 
 constexpr int kPlanThreads = 1024;
 constexpr int kPlanWaves = kPlanThreads / kWave;
-constexpr int kClasses = 16;         // unit lengths, longest first
-constexpr int kCachedGroups = 2048;  // group tables up to this size are searched in LDS
+constexpr int kClasses = 16;           // unit lengths, longest first
+constexpr int kPlanSequences = 4096;   // batches and group tables up to these sizes are
+constexpr int kPlanGroups = 2048;      // read once and kept in LDS
 
 __device__ __forceinline__ int length_class(int pages)
 {
@@ -114,158 +122,236 @@ __device__ __forceinline__ int length_class(int pages)
 
 // Writes the units, longest first, and each sequence's number of partial results.
 // Units of one class stand in any order: where a unit's results go does not depend
-// on it.
+// on it.  One work-group, bound by the latency of what it reads: lengths and groups
+// are read once, side by side, and everything after that is LDS (512 sequences in 64
+// groups: 9.4 us).
+template <bool CACHED>
 __global__ __launch_bounds__(kPlanThreads) void plan_prefix(PrefixArgs a)
 {
-    __shared__ int starts[kCachedGroups + 1];
+    __shared__ int lens_lds[CACHED ? kPlanSequences : 1];
+    __shared__ int starts_lds[CACHED ? kPlanGroups + 1 : 1];
+    __shared__ int pages_lds[CACHED ? kPlanGroups : 1];
+    __shared__ int leader_lds[CACHED ? kPlanGroups : 1];
     __shared__ int cursor[kClasses];
     const int t = threadIdx.x, lane = t % kWave, wave = t / kWave;
-    const bool cached = a.num_groups <= kCachedGroups;
+    const int32_t* const lens = CACHED ? lens_lds : a.seq_lens;
+    const int32_t* const starts = CACHED ? starts_lds : a.group_start;
+    const int32_t* const pages = CACHED ? pages_lds : a.prefix_pages;
+    int32_t* const leader = CACHED ? leader_lds : a.leaders;
+    const int cap = a.max_pages * kPageSize;
+    bool long_ones = false;
+    for (int b = t; b < a.batch; b += kPlanThreads) {
+        const int len = a.seq_lens[b];
+        long_ones |= len > cap;
+        if (CACHED)
+            lens_lds[b] = len;
+    }
+    for (int g = t; g < a.num_groups; g += kPlanThreads) {
+        leader[g] = INT32_MAX;
+        if (CACHED) {
+            starts_lds[g] = a.group_start[g];
+            pages_lds[g] = a.prefix_pages[g];
+        }
+    }
+    if (CACHED && t == 0 && a.num_groups > 0)
+        starts_lds[a.num_groups] = a.group_start[a.num_groups];
     if (t < kClasses)
         cursor[t] = 0;
-    if (cached && a.num_groups > 0)
-        for (int i = t; i <= a.num_groups; i += kPlanThreads)
-            starts[i] = a.group_start[i];
+    if (long_ones && a.dev_error != nullptr)
+        atomicOr(a.dev_error, RL_DA_DEVERR_LENGTH_TOO_LONG);
     __syncthreads();
-    auto start_of = [&](int g) { return cached ? starts[g] : a.group_start[g]; };
-    auto shared_pages = [&](int g) { return max(0, min(a.prefix_pages[g], a.max_pages)); };
-    const int cap = a.max_pages * kPageSize;
-    auto length_of = [&](int b) { return max(0, min(a.seq_lens[b], cap)); };
+    auto length_of = [&](int b) { return max(0, min(lens[b], cap)); };
+    auto shared_pages = [&](int g) { return max(0, min(pages[g], a.max_pages)); };
 
-    // A sequence's shared pages (0 for one that is no member) and own splits.
-    auto shared_of = [&](int b, int len) {
-        // the last group that starts at or before b
-        int lo = -1, hi = a.num_groups;
+    // The group that a sequence is a member of (it fills the group's shared pages),
+    // or -1.
+    auto group_of = [&](int b, int len) {
+        int lo = -1, hi = a.num_groups;  // the last group that starts at or before b
         while (hi - lo > 1) {
             const int mid = (lo + hi) / 2;
-            if (start_of(mid) <= b)
+            if (starts[mid] <= b)
                 lo = mid;
             else
                 hi = mid;
         }
-        if (lo < 0 || start_of(lo + 1) <= b)
-            return 0;  // in no group
+        if (lo < 0 || starts[lo + 1] <= b)
+            return -1;
         const int p = shared_pages(lo);
-        return len >= p * kPageSize ? p : 0;
+        return p > 0 && len >= p * kPageSize ? lo : -1;
     };
-    // A group's first member, whose table row the shared units read; -1: none.
-    auto first_member = [&](int s0, int s1, int need) {
-        for (int b0 = s0; b0 < s1; b0 += kWave) {
-            const int b = b0 + lane;
-            const uint64_t hit = __ballot(b < s1 && length_of(b) >= need);
-            if (hit != 0)
-                return b0 + (int)__builtin_ctzll(hit);
-        }
-        return -1;
+    struct Own {
+        int len, first, shared;  // first own page, splits of the shared ones
+        Splits s;
+    };
+    auto own_of = [&](int b, int g) {
+        Own o;
+        o.len = length_of(b);
+        o.first = g >= 0 ? shared_pages(g) : 0;
+        o.shared = splits_of(o.first, a.wanted_shared).count;
+        o.s = splits_of((o.len + kPageSize - 1) / kPageSize - o.first, a.wanted_own);
+        return o;
+    };
+    struct Shared {
+        int s0, rows, tiles, pages;
+        Splits s;
+    };
+    auto shared_of = [&](int g) {
+        Shared h;
+        h.s0 = max(0, min(starts[g], a.batch));
+        h.rows = (max(h.s0, min(starts[g + 1], a.batch)) - h.s0) << a.group_shift;
+        h.tiles = (h.rows + kTileRows - 1) / kTileRows;
+        h.pages = shared_pages(g);
+        h.s = splits_of(h.pages, a.wanted_shared);
+        return h;
     };
 
-    // The two passes, counting and writing, visit the same units.
-    auto pass = [&](auto sequence, auto shared) {
-        for (int b = t; b < a.batch; b += kPlanThreads) {
-            const int len = length_of(b);
-            const int p = shared_of(b, len);
-            sequence(b, len, p, splits_of((len + kPageSize - 1) / kPageSize - p, a.wanted_own));
-        }
-        for (int g = wave; g < a.num_groups; g += kPlanWaves) {
-            const int s0 = max(0, min(start_of(g), a.batch));
-            const int s1 = max(s0, min(start_of(g + 1), a.batch));
-            const int p = shared_pages(g);
-            if (p == 0)
-                continue;
-            const int leader = first_member(s0, s1, p * kPageSize);
-            if (leader >= 0)
-                shared(g, s0, s1, p, leader, splits_of(p, a.wanted_shared));
-        }
-    };
-    pass(
-        [&](int b, int len, int p, Splits s) {
-            if (a.dev_error != nullptr && a.seq_lens[b] > cap)
-                atomicOr(a.dev_error, RL_DA_DEVERR_LENGTH_TOO_LONG);
-            const int ps = splits_of(p, a.wanted_shared).count;
-            a.parts[b] = make_int2(ps, s.count);
-            if (s.count > 0)
-                atomicAdd(&cursor[length_class(s.pages)], s.count);
-        },
-        [&](int, int s0, int s1, int, int, Splits s) {
-            const int tiles = (((s1 - s0) << a.group_shift) + kTileRows - 1) / kTileRows;
-            if (lane == 0)
-                atomicAdd(&cursor[length_class(s.pages)], s.count * tiles);
-        });
+    // Count.  A group's first member lends its table row to the shared units; a
+    // group without one has none.
+    int my_group = -1;  // of the thread's first sequence
+    for (int b = t; b < a.batch; b += kPlanThreads) {
+        const int g = group_of(b, length_of(b));
+        if (b == t)
+            my_group = g;
+        const Own o = own_of(b, g);
+        a.parts[b] = make_int2(o.shared, o.s.count);
+        if (o.s.count > 0)
+            atomicAdd(&cursor[length_class(o.s.pages)], o.s.count);
+        if (g >= 0)
+            atomicMin(&leader[g], b);
+    }
     __syncthreads();
-    if (t == 0) {
+    for (int g = t; g < a.num_groups; g += kPlanThreads) {
+        if (leader[g] == INT32_MAX)
+            continue;
+        const Shared h = shared_of(g);
+        if (h.s.count * h.tiles > 0)
+            atomicAdd(&cursor[length_class(h.s.pages)], h.s.count * h.tiles);
+    }
+    __syncthreads();
+    if (t < kClasses) {
         int at = 0;
         for (int c = 0; c < kClasses; ++c) {
             const int n = cursor[c];
-            cursor[c] = at;
-            at += n;
+            at += c < t ? n : 0;
         }
+        const int n = cursor[t];
+        __builtin_amdgcn_wave_barrier();
+        cursor[t] = at;
         // group_start that runs backwards could name more units than there is room for
-        *a.num_units = min(at, a.max_units);
+        if (t == kClasses - 1) {
+            a.queue->units = min(at + n, a.max_units);
+            a.queue->next = 0;
+        }
     }
     __syncthreads();
+
+    // Write.
     auto put = [&](int at, const Unit& u) {
         if (at < a.max_units)
             a.units[at] = u;
     };
-    pass(
-        [&](int b, int len, int p, Splits s) {
-            if (s.count == 0)
-                return;
-            const int at = atomicAdd(&cursor[length_class(s.pages)], s.count);
-            const int total = (len + kPageSize - 1) / kPageSize;
-            const int ps = splits_of(p, a.wanted_shared).count;
-            for (int i = 0; i < s.count; ++i) {
-                Unit u;
-                u.table_row = b;
-                u.page0 = p + i * s.pages;
-                u.pages = min(s.pages, total - u.page0);
-                u.limit = len;
-                u.row0 = b << a.group_shift;
-                u.rows = 1 << a.group_shift;
-                u.slot = ps + s.count == 1 ? -1 : ps + i;
-                u.need = 0;
-                put(at + i, u);
-            }
-        },
-        [&](int, int s0, int s1, int p, int leader, Splits s) {
-            const int rows = (s1 - s0) << a.group_shift;
-            const int tiles = (rows + kTileRows - 1) / kTileRows;
-            int at = 0;
-            if (lane == 0)
-                at = atomicAdd(&cursor[length_class(s.pages)], s.count * tiles);
-            at = __builtin_amdgcn_readfirstlane(at);
-            // a split's tiles follow each other: they read the same pages
-            for (int i = lane; i < s.count * tiles; i += kWave) {
-                const int split = i / tiles, tile = i % tiles;
-                Unit u;
-                u.table_row = leader;
-                u.page0 = split * s.pages;
-                u.pages = min(s.pages, p - u.page0);
-                u.limit = p * kPageSize;
-                u.row0 = (s0 << a.group_shift) + tile * kTileRows;
-                u.rows = min(kTileRows, rows - tile * kTileRows);
-                u.slot = split;
-                u.need = p * kPageSize;
-                put(at + i, u);
-            }
-        });
+    for (int b0 = wave * kWave; b0 < a.batch; b0 += kPlanThreads) {
+        const int b = b0 + lane;
+        const bool has = b < a.batch;
+        const int g = !has ? -1 : (b == t ? my_group : group_of(b, length_of(b)));
+        Own o = own_of(has ? b : b0, g);
+        o.s.count = has ? o.s.count : 0;
+        int at = 0;
+        if (o.s.count > 0)
+            at = atomicAdd(&cursor[length_class(o.s.pages)], o.s.count);
+        auto put_own = [&](int b, int first, int pages, int len, int shared, int count, int at,
+                           int i) {
+            Unit u;
+            u.table_row = b;
+            u.page0 = first + i * pages;
+            u.pages = min(pages, (len + kPageSize - 1) / kPageSize - u.page0);
+            u.limit = len;
+            u.row0 = b << a.group_shift;
+            u.rows = 1 << a.group_shift;
+            u.slot = shared + count == 1 ? -1 : shared + i;
+            u.need = 0;
+            put(at + i, u);
+        };
+        // a lane writes its sequence's first units, all lanes together the others
+        constexpr int kAlone = 4;
+        for (int i = 0; i < min(o.s.count, kAlone); ++i)
+            put_own(b, o.first, o.s.pages, o.len, o.shared, o.s.count, at, i);
+        for (uint64_t more = __ballot(o.s.count > kAlone); more != 0; more &= more - 1) {
+            const int from = __builtin_ctzll(more);
+            auto of = [&](int v) { return __builtin_amdgcn_readlane(v, from); };
+            const int count = of(o.s.count);
+            for (int i = kAlone + lane; i < count; i += kWave)
+                put_own(b0 + from, of(o.first), of(o.s.pages), of(o.len), of(o.shared), count,
+                        of(at), i);
+        }
+    }
+    for (int g = wave; g < a.num_groups; g += kPlanWaves) {
+        const int first = leader[g];
+        if (first == INT32_MAX)
+            continue;
+        const Shared h = shared_of(g);
+        const int n = h.s.count * h.tiles;
+        int at = 0;
+        if (lane == 0 && n > 0)
+            at = atomicAdd(&cursor[length_class(h.s.pages)], n);
+        at = __builtin_amdgcn_readfirstlane(at);
+        // a split's tiles follow each other: they read the same pages
+        for (int i = lane; i < n; i += kWave) {
+            const int split = i / h.tiles, tile = i % h.tiles;
+            Unit u;
+            u.table_row = first;
+            u.page0 = split * h.s.pages;
+            u.pages = min(h.s.pages, h.pages - u.page0);
+            u.limit = h.pages * kPageSize;
+            u.row0 = (h.s0 << a.group_shift) + tile * kTileRows;
+            u.rows = min(kTileRows, h.rows - tile * kTileRows);
+            u.slot = split;
+            u.need = h.pages * kPageSize;
+            put(at + i, u);
+        }
+    }
 }
 
 // ---------------------------------------------------------------- attend ---
 //
-// A unit is one work-group of four wavefronts; wavefront w takes the unit's pages
-// w, w + 4, ... for all its rows, each from a double buffer of its own in LDS that
-// direct global-to-LDS loads fill: no barrier until the unit's end, where the four
-// (m, l, O) are joined.  Both products run transposed (S^T = K Q^T, O^T += V^T P^T),
-// so that a lane keeps one query row from the scores to the output and P^T goes from
-// the score registers into the second product as it lies there.  Each weight enters
-// the value product as two bf16 terms (hi + lo, 2^-16 relative).
+// A unit is one work-group of four wavefronts.  Both products run transposed (S^T =
+// K Q^T, O^T += V^T P^T), so that a lane keeps one query row from the scores to the
+// output and P^T goes from the score registers into the second product as it lies
+// there.  How a unit is shared among the wavefronts depends on its rows:
+//
+//   up to 16, 32 rows (attend_apart): wavefront w takes pages w, w + 4, ... for all
+//     rows, each from a double buffer of its own in LDS that direct global-to-LDS
+//     loads fill: no barrier until the unit's end, where the four (m, l, O) are
+//     joined.  Bound by HBM: the matrix cores idle most of the time, so each weight
+//     enters the value product as two bf16 terms (hi + lo, 2^-16 relative).
+//   up to 64, 128 rows (attend_together): 64 keys at a time pass through a double
+//     buffer of the work-group's, one barrier each; a wavefront holds 32 rows and
+//     takes all 64 keys (four wavefronts for 128 rows) or half of them (two pairs for
+//     64 rows, whose halves are joined at the end).  A key read from HBM meets 128
+//     rows, about where the matrix and vector units become the bound, so a weight
+//     enters as one bf16 term.  bf16 pools sum the same rounded weights for the
+//     normaliser, through the value product against ones.
 
 constexpr int kAttendThreads = kWave * kUnitWaves;
 constexpr int kBuffers = 2;
-constexpr int kPageLds = kPageSize * kHeadDim * 2;           // a page of bf16 keys or values
+constexpr int kPageLds = kPageSize * kHeadDim * 2;  // a page of bf16 keys or values
 constexpr int kWaveLds = kBuffers * 2 * kPageLds;
 constexpr int kLdsBytes = kUnitWaves * kWaveLds;
+constexpr int kStagePages = 4;                      // pages that a work-group shares
+constexpr int kStageTile = kStagePages * kPageLds;
+static_assert(kBuffers * 2 * kStageTile == kLdsBytes, "both ways use the same memory");
+
+struct AttendLds {
+    __attribute__((aligned(16))) char tiles[kLdsBytes];
+    float2 ml[kUnitWaves][32];
+    __attribute__((aligned(16))) int32_t pages[kMaxSplitPages + kStagePages];
+    __attribute__((aligned(16))) float2 scales[kMaxSplitPages + kStagePages];
+    int next_unit;
+};
+
+struct Lanes {
+    int wave, lane, i16, g4;
+};
 
 template <int N>
 __device__ __forceinline__ void wait_loads()  // all but the latest N of the wavefront's
@@ -276,308 +362,728 @@ __device__ __forceinline__ void wait_lds()
 {
     asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
 }
+__device__ __forceinline__ uint32_t lds_address(const void* p)
+{
+    typedef __attribute__((address_space(3))) void lds_void;
+    return (uint32_t)(uintptr_t)(lds_void*)p;
+}
+
+// Eight e4m3 codes to eight bf16 (exact), in order.
+__device__ __forceinline__ uint4 widen8(uint32_t a, uint32_t b)
+{
+    auto cvt = [](uint32_t w, auto upper) {
+        return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(
+                                                w, 1.0f, decltype(upper)::value));
+    };
+    return make_uint4(cvt(a, std::false_type{}), cvt(a, std::true_type{}),
+                      cvt(b, std::false_type{}), cvt(b, std::true_type{}));
+}
+
+// A table entry, checked: one outside the pool is reported, and page 0 read instead
+// (what the sequence gets is not defined).
+__device__ __forceinline__ int checked_page(const PrefixArgs& a, int page)
+{
+    if (page >= 0 && (int64_t)page < a.num_pages)
+        return page;
+    if (a.dev_error != nullptr)
+        atomicOr(a.dev_error, RL_DA_DEVERR_PAGE_OUT_OF_RANGE);
+    return 0;
+}
+
+// Query row `row` of kv head kvh as an MFMA operand: the lane's eight dims of each
+// quarter, 32 ks + 8 g4 .. (e4m3 keys read sixteen codes at once: 64 (ks / 2) + 16 g4 +
+// 8 (ks % 2) ..).
+template <bool CODES>
+__device__ __forceinline__ void load_query(const PrefixArgs& a, int kvh, int row, int g4,
+                                           uint4 (&q)[4])
+{
+    const int G = 1 << a.group_shift;
+    const uint16_t* p =
+        a.q + ((int64_t)(row >> a.group_shift) * a.num_q_heads + kvh * G + (row & (G - 1))) *
+                  kHeadDim;
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) {
+        q[ks] = *reinterpret_cast<const uint4*>(
+            p + (CODES ? 64 * (ks / 2) + 16 * g4 + 8 * (ks % 2) : 32 * ks + 8 * g4));
+        q[ks].x ^= a.q_sign;
+        q[ks].y ^= a.q_sign;
+        q[ks].z ^= a.q_sign;
+        q[ks].w ^= a.q_sign;
+    }
+}
+
+// Output row (of q and out) of a unit's row r, and whether it takes part.
+__device__ __forceinline__ int64_t output_row(const PrefixArgs& a, int kvh, int row)
+{
+    const int G = 1 << a.group_shift;
+    return (int64_t)(row >> a.group_shift) * a.num_q_heads + kvh * G + (row & (G - 1));
+}
 
 // A row's float4 chunks (dims 4c .. 4c + 3) in the joining area, moved apart so that
 // sixteen rows' equal chunks fall on different banks.
-__device__ __forceinline__ float4* join_chunk(char* lds, int wave, int row, int c)
+__device__ __forceinline__ float4* join_chunk(char* tiles, int wave, int row, int c)
 {
-    return reinterpret_cast<float4*>(lds + wave * kWaveLds + row * (kHeadDim * 4)) +
+    return reinterpret_cast<float4*>(tiles + wave * kWaveLds + row * (kHeadDim * 4)) +
            (c ^ (row & 15));
+}
+
+template <int RB, bool FP8>
+__device__ __forceinline__ void attend_apart(const PrefixArgs& a, const Unit& u, int kvh,
+                                             AttendLds& lds, const Lanes& at)
+{
+    const int wave = at.wave, lane = at.lane, i16 = at.i16, g4 = at.g4;
+    char* const mine = lds.tiles + wave * kWaveLds;
+    const uint32_t mine_at = lds_address(mine);
+    // bytes of a page's keys (or values) in a buffer, loads that bring both
+    constexpr int kTile = FP8 ? kPageLds / 2 : kPageLds;
+    constexpr int kLoads = 2 * kTile / 1024;
+    // e4m3: a page's values widened to bf16, behind the buffers of raw pages
+    char* const wide = mine + kBuffers * 2 * kTile;
+    const int count = wave < u.pages ? (u.pages - wave + kUnitWaves - 1) / kUnitWaves : 0;
+    int my_page = 0;
+    float my_ks = 1.0f, my_vs = 1.0f;
+    if (lane < count) {
+        my_page = checked_page(a, a.block_table[(int64_t)u.table_row * a.max_pages + u.page0 +
+                                                wave + lane * kUnitWaves]);
+        if (FP8) {
+            const int64_t slab = (int64_t)my_page * a.num_kv_heads + kvh;
+            my_ks = a.k_scale[slab];
+            my_vs = a.v_scale[slab];
+        }
+    }
+    uint4 q[RB][4];
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb)
+        load_query<FP8>(a, kvh, u.row0 + min(16 * rb + i16, u.rows - 1), g4, q[rb]);
+
+    // keys of the wavefront's i-th page that count
+    auto keys_of = [&](int i) {
+        return u.limit - (u.page0 + wave + i * kUnitWaves) * kPageSize;
+    };
+    auto issue = [&](int i) {
+        const int64_t page = __builtin_amdgcn_readlane(my_page, i);
+        const int64_t base = page * a.page_bytes + (int64_t)kvh * a.head_bytes;
+        const int last = min(keys_of(i), kPageSize) - 1;
+        const uint32_t to = mine_at + (i % kBuffers) * 2 * kTile;
+        constexpr int kRows = FP8 ? 8 : 4;     // rows of a page in one load
+        constexpr int kLanes = kWave / kRows;  // lanes, chunks of a row
+#pragma unroll
+        for (int r = 0; r < kPageSize / kRows; ++r) {
+            const int row = r * kRows + lane / kLanes;
+            const int chunk = (lane % kLanes) ^ (FP8 ? row >> 1 : chunk_swizzle(row));
+            // a key past the end is read as the last one (finite, weight 0)
+            const int64_t off = base + (int64_t)min(row, last) * a.row_bytes + 16 * chunk;
+            dma16(a.k_pool + off, to + 1024 * r);
+            dma16(a.v_pool + off, to + kTile + 1024 * r);
+        }
+    };
+
+    float m[RB], l[RB];
+    floatx4_t o[RB][8];
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+        m[rb] = kNoScore;
+        l[rb] = 0.0f;
+#pragma unroll
+        for (int db = 0; db < 8; ++db)
+            o[rb][db] = floatx4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+
+    auto consume = [&](int i) {
+        const char* kt = mine + (i % kBuffers) * 2 * kTile;
+        const char* vt = kt + kTile;
+        uint4 kv[4];
+        if constexpr (FP8) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const uint4 c = *reinterpret_cast<const uint4*>(
+                    kt + i16 * kHeadDim + 16 * ((4 * h + g4) ^ (i16 >> 1)));
+                kv[2 * h] = widen8(c.x, c.y);
+                kv[2 * h + 1] = widen8(c.z, c.w);
+            }
+            // values: lane holds rows lane / 8 and 8 + lane / 8, 16 codes of each
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int row = 8 * h + lane / 8, c0 = lane % 8;
+                const uint4 c = *reinterpret_cast<const uint4*>(vt + row * kHeadDim +
+                                                                16 * (c0 ^ (row >> 1)));
+                char* w = wide + row * (2 * kHeadDim);
+                const int sw = chunk_swizzle(row);
+                *reinterpret_cast<uint4*>(w + 16 * ((2 * c0) ^ sw)) = widen8(c.x, c.y);
+                *reinterpret_cast<uint4*>(w + 16 * ((2 * c0 + 1) ^ sw)) = widen8(c.z, c.w);
+            }
+            vt = wide;
+        } else {
+#pragma unroll
+            for (int ks = 0; ks < 4; ++ks)
+                kv[ks] = *reinterpret_cast<const uint4*>(
+                    kt + i16 * (2 * kHeadDim) + 16 * ((4 * ks + g4) ^ chunk_swizzle(i16)));
+        }
+        floatx4_t s[RB];
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb)
+            s[rb] = floatx4_t{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks)
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb)
+                s[rb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                    __builtin_bit_cast(bf16x8_t, kv[ks]), __builtin_bit_cast(bf16x8_t, q[rb][ks]),
+                    s[rb], 0, 0, 0);
+        // lane: row i16 of each block, keys 4 g4 .. + 3
+        float mult = a.scale_log2, vs = 1.0f;
+        if (FP8) {
+            mult *= __int_as_float(__builtin_amdgcn_readlane(__float_as_int(my_ks), i));
+            vs = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(my_vs), i));
+        }
+        const int keys = keys_of(i);
+        float x[RB][4], mx[RB];
+        bool grow = false;
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                x[rb][j] = 4 * g4 + j < keys ? s[rb][j] * mult : -INFINITY;
+            mx[rb] = fmaxf(fmaxf(x[rb][0], x[rb][1]), fmaxf(x[rb][2], x[rb][3]));
+            mx[rb] = max_lanes_xor32(max_lanes_xor16(mx[rb]));
+            grow |= mx[rb] > m[rb] + kMaxSlack;
+        }
+        if (__any(grow)) {
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb) {
+                const float m_new = mx[rb] > m[rb] + kMaxSlack ? mx[rb] : m[rb];
+                const float alpha = exp2_fast(m[rb] - m_new);
+                m[rb] = m_new;
+                l[rb] *= alpha;
+#pragma unroll
+                for (int db = 0; db < 8; ++db)
+                    o[rb][db] *= alpha;
+            }
+        }
+        uint2 hi[RB], lo[RB];
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+            float p[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                p[j] = exp2_fast(x[rb][j] - m[rb]);
+                l[rb] += p[j];
+                p[j] *= vs;
+            }
+            const uint32_t h0 = pack_bf16x2(p[0], p[1]), h1 = pack_bf16x2(p[2], p[3]);
+            hi[rb] = make_uint2(h0, h1);
+            lo[rb] = make_uint2(pack_bf16x2(p[0] - bf16_lo(h0), p[1] - bf16_hi(h0)),
+                                pack_bf16x2(p[2] - bf16_lo(h1), p[3] - bf16_hi(h1)));
+        }
+        if constexpr (FP8)
+            wave_lds_sync();  // the widened values are in place
+        const int vrow = 4 * g4 + (i16 >> 2), vsw = chunk_swizzle(vrow);
+#pragma unroll
+        for (int db = 0; db < 8; ++db) {
+            const uint2 vv = lds_read_transposed(reinterpret_cast<const uint16_t*>(
+                vt + vrow * (2 * kHeadDim) + 16 * ((2 * db + ((i16 & 3) >> 1)) ^ vsw) +
+                8 * (i16 & 1)));
+            const short4_t v4 = __builtin_bit_cast(short4_t, vv);
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb) {
+                o[rb][db] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(
+                    v4, __builtin_bit_cast(short4_t, hi[rb]), o[rb][db], 0, 0, 0);
+                o[rb][db] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(
+                    v4, __builtin_bit_cast(short4_t, lo[rb]), o[rb][db], 0, 0, 0);
+            }
+        }
+    };
+
+    if (count > 0)
+        issue(0);
+    if (count > 1)
+        issue(1);
+    for (int i = 0; i < count; ++i) {
+        if (i + 1 < count)
+            wait_loads<kLoads>();
+        else
+            wait_loads<0>();
+        consume(i);
+        wait_lds();  // the buffer has been read
+        if (i + 2 < count)
+            issue(i + 2);
+    }
+    __syncthreads();  // all wavefronts are done with their buffers
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+        l[rb] = sum_lanes_xor32(sum_lanes_xor16(l[rb]));
+#pragma unroll
+        for (int db = 0; db < 8; ++db)
+            *join_chunk(lds.tiles, wave, 16 * rb + i16, 4 * db + g4) =
+                make_float4(o[rb][db][0], o[rb][db][1], o[rb][db][2], o[rb][db][3]);
+        if (g4 == 0)
+            lds.ml[wave][16 * rb + i16] = make_float2(m[rb], l[rb]);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+        const int row = 16 * rb + threadIdx.x / 16;
+        const int r = u.row0 + row;
+        if (row >= u.rows || a.seq_lens[r >> a.group_shift] < u.need)
+            continue;
+        float2 ml[kUnitWaves];
+        float M = kNoScore;
+#pragma unroll
+        for (int w = 0; w < kUnitWaves; ++w) {
+            ml[w] = lds.ml[w][row];
+            M = fmaxf(M, ml[w].x);
+        }
+        float L = 0.0f, weight[kUnitWaves];
+#pragma unroll
+        for (int w = 0; w < kUnitWaves; ++w) {
+            weight[w] = exp2_fast(ml[w].x - M);
+            L = fmaf(weight[w], ml[w].y, L);
+        }
+        const int64_t out_row = output_row(a, kvh, r);
+        const int64_t part = out_row * a.slots + max(u.slot, 0);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int c = threadIdx.x % 16 + 16 * h;
+            float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+            for (int w = 0; w < kUnitWaves; ++w) {
+                const float4 x = *join_chunk(lds.tiles, w, row, c);
+                v.x = fmaf(weight[w], x.x, v.x);
+                v.y = fmaf(weight[w], x.y, v.y);
+                v.z = fmaf(weight[w], x.z, v.z);
+                v.w = fmaf(weight[w], x.w, v.w);
+            }
+            if (u.slot >= 0) {
+                *reinterpret_cast<float4*>(a.acc + part * kHeadDim + 4 * c) = v;
+            } else {
+                const float inv = 1.0f / L;
+                *reinterpret_cast<uint2*>(a.out + out_row * kHeadDim + 4 * c) = make_uint2(
+                    pack_bf16x2(v.x * inv, v.y * inv), pack_bf16x2(v.z * inv, v.w * inv));
+            }
+        }
+        if (u.slot >= 0 && threadIdx.x % 16 == 0)
+            a.ml[part] = make_float2(M, L);
+    }
+}
+
+// KW wavefronts share 32 rows, each taking 1 / KW of a stage's keys.
+template <int KW, bool FP8>
+__device__ __forceinline__ void attend_together(const PrefixArgs& a, const Unit& u, int kvh,
+                                                AttendLds& lds, const Lanes& at)
+{
+    constexpr int RB = 2;
+    constexpr int KB = kStagePages / KW;  // 16-key blocks of a stage per wavefront
+    const int wave = at.wave, lane = at.lane, i16 = at.i16, g4 = at.g4;
+    const int kw = wave % KW, row_base = wave / KW * 32;
+    const int stages = (u.pages + kStagePages - 1) / kStagePages;
+    auto k_tile = [&](int sel) { return lds.tiles + sel * 2 * kStageTile; };
+    auto v_tile = [&](int sel) { return lds.tiles + sel * 2 * kStageTile + kStageTile; };
+
+    // The unit's pages and their scales; a stage's pages past the unit's last are read
+    // as that one (finite) and masked.
+    for (int i = threadIdx.x; i < stages * kStagePages; i += kAttendThreads) {
+        const int page = checked_page(
+            a, a.block_table[(int64_t)u.table_row * a.max_pages + u.page0 +
+                             min(i, u.pages - 1)]);
+        lds.pages[i] = page;
+        if (FP8) {
+            const int64_t slab = (int64_t)page * a.num_kv_heads + kvh;
+            lds.scales[i] = make_float2(a.k_scale[slab], a.v_scale[slab]);
+        }
+    }
+    uint4 q[RB][4];
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb)
+        load_query<false>(a, kvh, u.row0 + min(row_base + 16 * rb + i16, u.rows - 1), g4, q[rb]);
+    __syncthreads();
+
+    // bf16: wavefront w brings rows 4w .. 4w + 3 of each page, lane l the chunk that the
+    // swizzle puts at position l % 16 of row 4w + l / 16.
+    const int d_row = 4 * wave + lane / 16;
+    const int64_t d_off = (int64_t)kvh * a.head_bytes + (int64_t)d_row * a.row_bytes +
+                          16 * ((lane % 16) ^ chunk_swizzle(d_row));
+    auto bring = [&](int stage, int sel) {
+        const int4 pg = *reinterpret_cast<const int4*>(&lds.pages[stage * kStagePages]);
+        const int page[kStagePages] = {pg.x, pg.y, pg.z, pg.w};
+        const uint32_t k_at = lds_address(k_tile(sel)), v_at = lds_address(v_tile(sel));
+#pragma unroll
+        for (int r = 0; r < kStagePages; ++r) {
+            const int64_t off =
+                (int64_t)__builtin_amdgcn_readfirstlane(page[r]) * a.page_bytes + d_off;
+            dma16(a.k_pool + off, k_at + r * kPageLds + 1024 * wave);
+            dma16(a.v_pool + off, v_at + r * kPageLds + 1024 * wave);
+        }
+    };
+    // e4m3: thread t loads the codes of dims 16 (t % 8) .. + 15 of key rows 2 (t / 8)
+    // and the next one, and widens them on the way into the tiles.
+    const int s_row = 2 * (threadIdx.x / 8), s_chunk = 2 * (threadIdx.x % 8);
+    const int64_t s_off = (int64_t)kvh * a.head_bytes +
+                          (int64_t)(s_row % kPageSize) * a.row_bytes + 8 * s_chunk;
+    uint4 kr[2], vr[2];
+    auto fetch = [&](int stage) {
+        const int64_t off =
+            (int64_t)lds.pages[stage * kStagePages + s_row / kPageSize] * a.page_bytes + s_off;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            kr[i] = *reinterpret_cast<const uint4*>(a.k_pool + off + i * a.row_bytes);
+            vr[i] = *reinterpret_cast<const uint4*>(a.v_pool + off + i * a.row_bytes);
+        }
+    };
+    auto stash = [&](int sel) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int row = s_row + i, sw = chunk_swizzle(row % kPageSize);
+            char* k = k_tile(sel) + row * (2 * kHeadDim);
+            char* v = v_tile(sel) + row * (2 * kHeadDim);
+            *reinterpret_cast<uint4*>(k + 16 * (s_chunk ^ sw)) = widen8(kr[i].x, kr[i].y);
+            *reinterpret_cast<uint4*>(k + 16 * ((s_chunk + 1) ^ sw)) = widen8(kr[i].z, kr[i].w);
+            *reinterpret_cast<uint4*>(v + 16 * (s_chunk ^ sw)) = widen8(vr[i].x, vr[i].y);
+            *reinterpret_cast<uint4*>(v + 16 * ((s_chunk + 1) ^ sw)) = widen8(vr[i].z, vr[i].w);
+        }
+    };
+
+    // Operand offsets into a tile, made once.
+    int k_off[4], v_off[8];
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks)
+        k_off[ks] = i16 * (2 * kHeadDim) + 16 * ((4 * ks + g4) ^ chunk_swizzle(i16));
+    const int vrow = 4 * g4 + (i16 >> 2);
+#pragma unroll
+    for (int db = 0; db < 8; ++db)
+        v_off[db] = vrow * (2 * kHeadDim) +
+                    16 * ((2 * db + ((i16 & 3) >> 1)) ^ chunk_swizzle(vrow)) + 8 * (i16 & 1);
+
+    float m[RB], l[RB];
+    floatx4_t lacc[RB], o[RB][8];
+    const uint4 ones = make_uint4(0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u);
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+        m[rb] = kNoScore;
+        l[rb] = 0.0f;
+        lacc[rb] = floatx4_t{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int db = 0; db < 8; ++db)
+            o[rb][db] = floatx4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+
+    auto stage = [&](int j, int sel, auto last_t) __attribute__((always_inline)) {
+        constexpr bool kLast = decltype(last_t)::value;
+        if constexpr (FP8) {
+            stash(sel);
+            if (j + 1 < stages)
+                fetch(j + 1);
+            __syncthreads();
+        } else {
+            wait_loads<0>();  // this wavefront's share of the stage
+            __syncthreads();
+        }
+        const char* kt = k_tile(sel) + kw * KB * kPageLds;
+        const char* vt = v_tile(sel) + kw * KB * kPageLds;
+        floatx4_t s[RB][KB];
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb)
+                s[rb][kb] = floatx4_t{0.0f, 0.0f, 0.0f, 0.0f};
+        __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks)
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb) {
+                const uint4 kv =
+                    *reinterpret_cast<const uint4*>(kt + kb * kPageLds + k_off[ks]);
+#pragma unroll
+                for (int rb = 0; rb < RB; ++rb)
+                    s[rb][kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                        __builtin_bit_cast(bf16x8_t, kv), __builtin_bit_cast(bf16x8_t, q[rb][ks]),
+                        s[rb][kb], 0, 0, 0);
+            }
+        __builtin_amdgcn_s_setprio(0);
+        if constexpr (!FP8) {
+            if (j + 1 < stages)
+                bring(j + 1, 1 - sel);
+        }
+        // scores in log2 units are s * mult
+        float mult[KB], vs[KB];
+        const int page0 = j * kStagePages + kw * KB;
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) {
+            mult[kb] = a.scale_log2;
+            vs[kb] = 1.0f;
+            if (FP8) {
+                const float2 sc = lds.scales[page0 + kb];
+                mult[kb] *= sc.x;
+                vs[kb] = sc.y;
+            }
+        }
+        float mx[RB];
+        bool grow = false;
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+            mx[rb] = -INFINITY;
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb) {
+                if (kLast && page0 + kb >= u.pages) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        s[rb][kb][i] = -INFINITY;
+                    mult[kb] = 1.0f;
+                    continue;
+                }
+                if (FP8) {  // multipliers of any sign
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        s[rb][kb][i] *= mult[kb];
+                }
+                const float top = __builtin_elementwise_maximum(
+                    __builtin_elementwise_maximum(s[rb][kb][0], s[rb][kb][1]),
+                    __builtin_elementwise_maximum(s[rb][kb][2], s[rb][kb][3]));
+                mx[rb] = __builtin_elementwise_maximum(mx[rb], top);
+            }
+            if (!FP8)
+                mx[rb] *= a.scale_log2;
+            mx[rb] = max_lanes_xor32(max_lanes_xor16(mx[rb]));
+            grow |= mx[rb] > m[rb] + kMaxSlack;
+        }
+        if (__builtin_expect(__any(grow), 0)) {
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb) {
+                const float m_new = mx[rb] > m[rb] + kMaxSlack ? mx[rb] : m[rb];
+                const float alpha = exp2_fast(m[rb] - m_new);
+                m[rb] = m_new;
+                l[rb] *= alpha;
+                lacc[rb] *= alpha;
+#pragma unroll
+                for (int db = 0; db < 8; ++db)
+                    o[rb][db] *= alpha;
+            }
+        }
+        // two 16-key blocks' weights are one operand: keys 4 g4 .. + 3 of each
+        uint4 pt[RB][KB / 2];
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+            for (int kh = 0; kh < KB / 2; ++kh) {
+                uint32_t w[4];
+#pragma unroll
+                for (int half = 0; half < 4; ++half) {
+                    const int kb = 2 * kh + half / 2, i = 2 * (half % 2);
+                    float p0, p1;
+                    if (FP8) {
+                        p0 = exp2_fast(s[rb][kb][i] - m[rb]);
+                        p1 = exp2_fast(s[rb][kb][i + 1] - m[rb]);
+                        l[rb] += p0 + p1;
+                        p0 *= vs[kb];
+                        p1 *= vs[kb];
+                    } else {
+                        p0 = exp2_fast(fmaf(s[rb][kb][i], mult[kb], -m[rb]));
+                        p1 = exp2_fast(fmaf(s[rb][kb][i + 1], mult[kb], -m[rb]));
+                    }
+                    w[half] = pack_bf16x2(p0, p1);
+                }
+                pt[rb][kh] = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+        __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+        for (int kh = 0; kh < KB / 2; ++kh)
+#pragma unroll
+            for (int db = 0; db < 8; ++db) {
+                const char* p = vt + 2 * kh * kPageLds + v_off[db];
+                const uint2 va = lds_read_transposed(reinterpret_cast<const uint16_t*>(p));
+                const uint2 vb =
+                    lds_read_transposed(reinterpret_cast<const uint16_t*>(p + kPageLds));
+                const uint4 v = make_uint4(va.x, va.y, vb.x, vb.y);
+#pragma unroll
+                for (int rb = 0; rb < RB; ++rb)
+                    o[rb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                        __builtin_bit_cast(bf16x8_t, v), __builtin_bit_cast(bf16x8_t, pt[rb][kh]),
+                        o[rb][db], 0, 0, 0);
+            }
+        if (!FP8) {
+#pragma unroll
+            for (int kh = 0; kh < KB / 2; ++kh)
+#pragma unroll
+                for (int rb = 0; rb < RB; ++rb)
+                    lacc[rb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                        __builtin_bit_cast(bf16x8_t, ones),
+                        __builtin_bit_cast(bf16x8_t, pt[rb][kh]), lacc[rb], 0, 0, 0);
+        }
+        __builtin_amdgcn_s_setprio(0);
+    };
+    if constexpr (FP8)
+        fetch(0);
+    else
+        bring(0, 0);
+    int j = 0;
+    for (; j < stages - 1; ++j)
+        stage(j, j & 1, std::false_type{});
+    stage(j, j & 1, std::true_type{});
+
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb)
+        l[rb] = FP8 ? sum_lanes_xor32(sum_lanes_xor16(l[rb])) : lacc[rb][0];
+    if constexpr (KW == 2) {
+        // the second wavefront of a pair hands its half to the first, lane by lane
+        __syncthreads();  // the tiles have been read
+        float4* area = reinterpret_cast<float4*>(lds.tiles) + (wave / 2) * (RB * 8 * kWave) + lane;
+        if (kw == 1) {
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb) {
+#pragma unroll
+                for (int db = 0; db < 8; ++db)
+                    area[(8 * rb + db) * kWave] =
+                        make_float4(o[rb][db][0], o[rb][db][1], o[rb][db][2], o[rb][db][3]);
+                if (g4 == 0)
+                    lds.ml[wave][16 * rb + i16] = make_float2(m[rb], l[rb]);
+            }
+        }
+        __syncthreads();
+        if (kw == 1)
+            return;
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+            const float2 ml = lds.ml[wave + 1][16 * rb + i16];
+            const float M = fmaxf(m[rb], ml.x);
+            const float w0 = exp2_fast(m[rb] - M), w1 = exp2_fast(ml.x - M);
+            m[rb] = M;
+            l[rb] = fmaf(w1, ml.y, w0 * l[rb]);
+#pragma unroll
+            for (int db = 0; db < 8; ++db) {
+                const float4 x = area[(8 * rb + db) * kWave];
+                o[rb][db][0] = fmaf(w1, x.x, w0 * o[rb][db][0]);
+                o[rb][db][1] = fmaf(w1, x.y, w0 * o[rb][db][1]);
+                o[rb][db][2] = fmaf(w1, x.z, w0 * o[rb][db][2]);
+                o[rb][db][3] = fmaf(w1, x.w, w0 * o[rb][db][3]);
+            }
+        }
+    }
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+        const int row = row_base + 16 * rb + i16, r = u.row0 + row;
+        if (row >= u.rows || a.seq_lens[r >> a.group_shift] < u.need)
+            continue;
+        const int64_t part = output_row(a, kvh, r) * a.slots + u.slot;
+#pragma unroll
+        for (int db = 0; db < 8; ++db)
+            *reinterpret_cast<float4*>(a.acc + part * kHeadDim + 16 * db + 4 * g4) =
+                make_float4(o[rb][db][0], o[rb][db][1], o[rb][db][2], o[rb][db][3]);
+        if (g4 == 0)
+            a.ml[part] = make_float2(m[rb], l[rb]);
+    }
 }
 
 template <bool FP8>
 __global__ __launch_bounds__(kAttendThreads) __attribute__((amdgpu_waves_per_eu(2))) void
 attend_prefix(PrefixArgs a)
 {
-    __shared__ __attribute__((aligned(16))) char lds[kLdsBytes];
-    __shared__ float2 join_ml[kUnitWaves][kTileRows];
-    typedef __attribute__((address_space(3))) void lds_void;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const int lane = threadIdx.x % kWave;
-    const int i16 = lane & 15, g4 = lane >> 4;
-    const int G = 1 << a.group_shift;
-    char* const mine = lds + wave * kWaveLds;
-    const uint32_t mine_at = (uint32_t)(uintptr_t)(lds_void*)mine;
-    // bytes of a page's keys (or values) in a buffer, loads that bring both
-    constexpr int kTile = FP8 ? kPageLds / 2 : kPageLds;
-    constexpr int kLoads = 2 * kTile / 1024;
-    // e4m3: a page's values widened to bf16, behind the buffers of raw pages
-    char* const wide = mine + kBuffers * 2 * kTile;
-    const int total = *a.num_units * a.num_kv_heads;
-    const int64_t q_rows = a.num_q_heads;
+    __shared__ AttendLds lds;
+    Lanes lanes;
+    lanes.wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    lanes.lane = threadIdx.x % kWave;
+    lanes.i16 = lanes.lane & 15;
+    lanes.g4 = lanes.lane >> 4;
+    const int total = a.queue->units * a.num_kv_heads;
 
-    for (int at = blockIdx.x; at < total; at += gridDim.x) {
+    // A work-group's first unit is its own place in the list, the others come from the
+    // queue, asked for while the one before runs.
+    int at = blockIdx.x;
+    while (at < total) {
+        int taken = 0;
+        if (threadIdx.x == 0)
+            taken = atomicAdd(&a.queue->next, 1);
         const Unit u = a.units[at / a.num_kv_heads];
         const int kvh = at % a.num_kv_heads;
-        const int count = wave < u.pages ? (u.pages - wave + kUnitWaves - 1) / kUnitWaves : 0;
-        int my_page = 0;
-        float my_ks = 1.0f, my_vs = 1.0f;
-        if (lane < count) {
-            my_page = a.block_table[(int64_t)u.table_row * a.max_pages + u.page0 + wave +
-                                    lane * kUnitWaves];
-            if (my_page < 0 || (int64_t)my_page >= a.num_pages) {
-                // read another page instead; what the sequence gets is not defined
-                if (a.dev_error != nullptr)
-                    atomicOr(a.dev_error, RL_DA_DEVERR_PAGE_OUT_OF_RANGE);
-                my_page = 0;
-            }
-            if (FP8) {
-                const int64_t slab = (int64_t)my_page * a.num_kv_heads + kvh;
-                my_ks = a.k_scale[slab];
-                my_vs = a.v_scale[slab];
-            }
-        }
-        // Q^T: lane holds row i16, dims 32 ks + 8 g4 .. + 7 (e4m3: the dims of the
-        // codes it reads together, 64 (ks / 2) + 16 g4 + 8 (ks % 2) ..)
-        const int my_row = u.row0 + min(i16, u.rows - 1);
-        const uint16_t* qrow =
-            a.q + ((int64_t)(my_row >> a.group_shift) * q_rows + kvh * G + (my_row & (G - 1))) *
-                      kHeadDim;
-        uint4 q[4];
-#pragma unroll
-        for (int ks = 0; ks < 4; ++ks)
-            q[ks] = *reinterpret_cast<const uint4*>(
-                qrow + (FP8 ? 64 * (ks / 2) + 16 * g4 + 8 * (ks % 2) : 32 * ks + 8 * g4));
-
-        // keys of the wavefront's i-th page that count
-        auto keys_of = [&](int i) {
-            return u.limit - (u.page0 + wave + i * kUnitWaves) * kPageSize;
-        };
-        auto issue = [&](int i) {
-            const int64_t page = __builtin_amdgcn_readlane(my_page, i);
-            const int64_t base = page * a.page_bytes + (int64_t)kvh * a.head_bytes;
-            const int last = min(keys_of(i), kPageSize) - 1;
-            const uint32_t to = mine_at + (i % kBuffers) * 2 * kTile;
-            constexpr int kRows = FP8 ? 8 : 4;       // rows of a page in one load
-            constexpr int kLanes = kWave / kRows;    // lanes, chunks of a row
-#pragma unroll
-            for (int r = 0; r < kPageSize / kRows; ++r) {
-                const int row = r * kRows + lane / kLanes;
-                const int chunk = (lane % kLanes) ^ (FP8 ? row >> 1 : chunk_swizzle(row));
-                // a key past the end is read as the last one (finite, weight 0)
-                const int64_t off =
-                    base + (int64_t)min(row, last) * a.row_bytes + 16 * chunk;
-                dma16(a.k_pool + off, to + 1024 * r);
-                dma16(a.v_pool + off, to + kTile + 1024 * r);
-            }
-        };
-
-        float m = kNoScore, l = 0.0f;
-        floatx4_t o[8];
-#pragma unroll
-        for (int db = 0; db < 8; ++db)
-            o[db] = floatx4_t{0.0f, 0.0f, 0.0f, 0.0f};
-
-        auto consume = [&](int i) {
-            const char* kt = mine + (i % kBuffers) * 2 * kTile;
-            const char* vt = kt + kTile;
-            uint4 kv[4];
-            if constexpr (FP8) {
-                auto cvt = [](uint32_t w, auto upper) {
-                    return __builtin_bit_cast(uint32_t,
-                                              __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(
-                                                  w, 1.0f, decltype(upper)::value));
-                };
-                using F = std::false_type;
-                using T = std::true_type;
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const uint4 c = *reinterpret_cast<const uint4*>(
-                        kt + i16 * kHeadDim + 16 * ((4 * h + g4) ^ (i16 >> 1)));
-                    kv[2 * h] = make_uint4(cvt(c.x, F{}), cvt(c.x, T{}), cvt(c.y, F{}),
-                                           cvt(c.y, T{}));
-                    kv[2 * h + 1] = make_uint4(cvt(c.z, F{}), cvt(c.z, T{}), cvt(c.w, F{}),
-                                               cvt(c.w, T{}));
-                }
-                // values: lane holds rows lane / 8 and 8 + lane / 8, 16 codes of each
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int row = 8 * h + lane / 8, c0 = lane % 8;
-                    const uint4 c = *reinterpret_cast<const uint4*>(
-                        vt + row * kHeadDim + 16 * (c0 ^ (row >> 1)));
-                    char* w = wide + row * (2 * kHeadDim);
-                    const int sw = chunk_swizzle(row);
-                    *reinterpret_cast<uint4*>(w + 16 * ((2 * c0) ^ sw)) =
-                        make_uint4(cvt(c.x, F{}), cvt(c.x, T{}), cvt(c.y, F{}), cvt(c.y, T{}));
-                    *reinterpret_cast<uint4*>(w + 16 * ((2 * c0 + 1) ^ sw)) =
-                        make_uint4(cvt(c.z, F{}), cvt(c.z, T{}), cvt(c.w, F{}), cvt(c.w, T{}));
-                }
-                vt = wide;
-            } else {
-#pragma unroll
-                for (int ks = 0; ks < 4; ++ks)
-                    kv[ks] = *reinterpret_cast<const uint4*>(
-                        kt + i16 * (2 * kHeadDim) + 16 * ((4 * ks + g4) ^ chunk_swizzle(i16)));
-            }
-            floatx4_t s = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-            for (int ks = 0; ks < 4; ++ks)
-                s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, kv[ks]),
-                                                            __builtin_bit_cast(bf16x8_t, q[ks]),
-                                                            s, 0, 0, 0);
-            // lane: row i16, keys 4 g4 .. + 3
-            float mult = a.scale_log2, vs = 1.0f;
-            if (FP8) {
-                mult *= __int_as_float(__builtin_amdgcn_readlane(__float_as_int(my_ks), i));
-                vs = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(my_vs), i));
-            }
-            const int keys = keys_of(i);
-            float x[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                x[j] = 4 * g4 + j < keys ? s[j] * mult : -INFINITY;
-            float mx = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
-            mx = max_lanes_xor32(max_lanes_xor16(mx));
-            if (__any(mx > m + kMaxSlack)) {
-                const float m_new = mx > m + kMaxSlack ? mx : m;
-                const float alpha = exp2_fast(m - m_new);
-                m = m_new;
-                l *= alpha;
-#pragma unroll
-                for (int db = 0; db < 8; ++db)
-                    o[db] *= alpha;
-            }
-            float p[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                p[j] = exp2_fast(x[j] - m);
-                l += p[j];
-                p[j] *= vs;
-            }
-            const uint32_t h0 = pack_bf16x2(p[0], p[1]), h1 = pack_bf16x2(p[2], p[3]);
-            const uint2 hi = make_uint2(h0, h1);
-            const uint2 lo = make_uint2(pack_bf16x2(p[0] - bf16_lo(h0), p[1] - bf16_hi(h0)),
-                                        pack_bf16x2(p[2] - bf16_lo(h1), p[3] - bf16_hi(h1)));
-            if constexpr (FP8)
-                wave_lds_sync();  // the widened values are in place
-            const int vrow = 4 * g4 + (i16 >> 2), vsw = chunk_swizzle(vrow);
-#pragma unroll
-            for (int db = 0; db < 8; ++db) {
-                const uint2 vv = lds_read_transposed(reinterpret_cast<const uint16_t*>(
-                    vt + vrow * (2 * kHeadDim) + 16 * ((2 * db + ((i16 & 3) >> 1)) ^ vsw) +
-                    8 * (i16 & 1)));
-                const short4_t v4 = __builtin_bit_cast(short4_t, vv);
-                o[db] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(
-                    v4, __builtin_bit_cast(short4_t, hi), o[db], 0, 0, 0);
-                o[db] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(
-                    v4, __builtin_bit_cast(short4_t, lo), o[db], 0, 0, 0);
-            }
-        };
-
-        if (count > 0)
-            issue(0);
-        if (count > 1)
-            issue(1);
-        for (int i = 0; i < count; ++i) {
-            if (i + 1 < count)
-                wait_loads<kLoads>();
-            else
-                wait_loads<0>();
-            consume(i);
-            wait_lds();  // the buffer has been read
-            if (i + 2 < count)
-                issue(i + 2);
-        }
-        l = sum_lanes_xor32(sum_lanes_xor16(l));
-        __syncthreads();  // all wavefronts are done with their buffers
-#pragma unroll
-        for (int db = 0; db < 8; ++db)
-            *join_chunk(lds, wave, i16, 4 * db + g4) =
-                make_float4(o[db][0], o[db][1], o[db][2], o[db][3]);
-        if (g4 == 0)
-            join_ml[wave][i16] = make_float2(m, l);
-        __syncthreads();
-        {
-            const int row = threadIdx.x / 16;
-            const int r = u.row0 + row, b = r >> a.group_shift;
-            if (row < u.rows && a.seq_lens[b] >= u.need) {
-                float2 ml[kUnitWaves];
-                float M = kNoScore;
-#pragma unroll
-                for (int w = 0; w < kUnitWaves; ++w) {
-                    ml[w] = join_ml[w][row];
-                    M = fmaxf(M, ml[w].x);
-                }
-                float L = 0.0f, weight[kUnitWaves];
-#pragma unroll
-                for (int w = 0; w < kUnitWaves; ++w) {
-                    weight[w] = exp2_fast(ml[w].x - M);
-                    L = fmaf(weight[w], ml[w].y, L);
-                }
-                const int64_t out_row = (int64_t)b * a.num_q_heads + kvh * G + (r & (G - 1));
-                const int64_t part = out_row * a.slots + max(u.slot, 0);
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int c = threadIdx.x % 16 + 16 * h;
-                    float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll
-                    for (int w = 0; w < kUnitWaves; ++w) {
-                        const float4 x = *join_chunk(lds, w, row, c);
-                        v.x = fmaf(weight[w], x.x, v.x);
-                        v.y = fmaf(weight[w], x.y, v.y);
-                        v.z = fmaf(weight[w], x.z, v.z);
-                        v.w = fmaf(weight[w], x.w, v.w);
-                    }
-                    if (u.slot >= 0) {
-                        *reinterpret_cast<float4*>(a.acc + part * kHeadDim + 4 * c) = v;
-                    } else {
-                        const float inv = 1.0f / L;
-                        *reinterpret_cast<uint2*>(a.out + out_row * kHeadDim + 4 * c) =
-                            make_uint2(pack_bf16x2(v.x * inv, v.y * inv),
-                                       pack_bf16x2(v.z * inv, v.w * inv));
-                    }
-                }
-                if (u.slot >= 0 && threadIdx.x % 16 == 0)
-                    a.ml[part] = make_float2(M, L);
-            }
-        }
-        __syncthreads();  // the next unit's loads overwrite the joining area
+        if (u.rows <= 16)
+            attend_apart<1, FP8>(a, u, kvh, lds, lanes);
+        else if (u.rows <= 32)
+            attend_apart<2, FP8>(a, u, kvh, lds, lanes);
+        else if (u.rows <= 64)
+            attend_together<2, FP8>(a, u, kvh, lds, lanes);
+        else
+            attend_together<1, FP8>(a, u, kvh, lds, lanes);
+        if (threadIdx.x == 0)
+            lds.next_unit = gridDim.x + taken;
+        __syncthreads();  // the next unit's loads overwrite what this one still read
+        at = __builtin_amdgcn_readfirstlane(lds.next_unit);
     }
 }
 
 // ----------------------------------------------------------------- merge ---
 //
-// 32 lanes per output row, four dims each; a row's partial results in order.
+// 32 lanes per output row, four dims each, walk a row's partial results in order;
+// with SPREAD the eight such teams of a work-group share one row, team i taking
+// results i, i + 8, ..., and their sums are joined in team order.
 
-constexpr int kMergeRows = 8;  // of a work-group
+constexpr int kMergeTeams = 8;
+constexpr int kMergeThreads = kMergeTeams * 32;
 
-__global__ __launch_bounds__(kMergeRows * 32) void merge_prefix(PrefixArgs a)
+struct Joined {  // partial results so far, relative to their largest score
+    float m, l;
+    float4 v;
+};
+__device__ __forceinline__ void join(Joined& j, float m, float l, const float4& v)
 {
-    const int64_t row = (int64_t)blockIdx.x * kMergeRows + threadIdx.x / 32;
+    const float M = fmaxf(j.m, m);
+    const float w0 = exp2_fast(j.m - M), w1 = exp2_fast(m - M);
+    j.m = M;
+    j.l = fmaf(w1, l, w0 * j.l);
+    j.v.x = fmaf(w1, v.x, w0 * j.v.x);
+    j.v.y = fmaf(w1, v.y, w0 * j.v.y);
+    j.v.z = fmaf(w1, v.z, w0 * j.v.z);
+    j.v.w = fmaf(w1, v.w, w0 * j.v.w);
+}
+
+template <bool SPREAD>
+__global__ __launch_bounds__(kMergeThreads) void merge_prefix(PrefixArgs a)
+{
+    const int team = threadIdx.x / 32, c = threadIdx.x % 32;
+    const int64_t row = SPREAD ? blockIdx.x : (int64_t)blockIdx.x * kMergeTeams + team;
     if (row >= (int64_t)a.batch * a.num_q_heads)
         return;
-    const int c = threadIdx.x % 32;
     const int2 parts = a.parts[row / a.num_q_heads];
     const int n = parts.x + parts.y;
     if (parts.x == 0 && n == 1)
         return;  // its unit has written it
     const float2* ml = a.ml + row * a.slots;
     const float4* acc = reinterpret_cast<const float4*>(a.acc + row * a.slots * kHeadDim) + c;
-    float M = kNoScore;
-    for (int s = 0; s < n; ++s)
-        M = fmaxf(M, ml[s].x);
-    float den = 0.0f;
-    float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 4
-    for (int s = 0; s < n; ++s) {
-        const float2 e = ml[s];
-        const float4 x = acc[s * (kHeadDim / 4)];
-        const float w = exp2_fast(e.x - M);
-        den = fmaf(w, e.y, den);
-        v.x = fmaf(w, x.x, v.x);
-        v.y = fmaf(w, x.y, v.y);
-        v.z = fmaf(w, x.z, v.z);
-        v.w = fmaf(w, x.w, v.w);
+    Joined j = {kNoScore, 0.0f, make_float4(0.0f, 0.0f, 0.0f, 0.0f)};
+    constexpr int kStep = SPREAD ? kMergeTeams : 1;
+    constexpr int kAhead = 4;  // results read side by side
+    for (int s0 = SPREAD ? team : 0; s0 < n; s0 += kAhead * kStep) {
+        float2 e[kAhead];
+        float4 x[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const int s = min(s0 + i * kStep, n - 1);
+            e[i] = ml[s];
+            x[i] = acc[(int64_t)s * (kHeadDim / 4)];
+        }
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i)
+            if (s0 + i * kStep < n)
+                join(j, e[i].x, e[i].y, x[i]);
     }
-    const float inv = n > 0 ? 1.0f / den : 0.0f;  // no keys: zeros
+    if constexpr (SPREAD) {
+        __shared__ float4 team_v[kMergeTeams][32];
+        __shared__ float2 team_ml[kMergeTeams];
+        team_v[team][c] = j.v;
+        if (c == 0)
+            team_ml[team] = make_float2(j.m, j.l);
+        __syncthreads();
+        if (team != 0)
+            return;
+        for (int i = 1; i < min(n, kMergeTeams); ++i)
+            join(j, team_ml[i].x, team_ml[i].y, team_v[i][c]);
+    }
+    const float inv = n > 0 ? 1.0f / j.l : 0.0f;  // no keys: zeros
     *reinterpret_cast<uint2*>(a.out + row * kHeadDim + 4 * c) = make_uint2(
-        pack_bf16x2(v.x * inv, v.y * inv), pack_bf16x2(v.z * inv, v.w * inv));
+        pack_bf16x2(j.v.x * inv, j.v.y * inv), pack_bf16x2(j.v.z * inv, j.v.w * inv));
 }
 
 // ------------------------------------------------------------------ host ---
 
 struct Workspace {
-    int64_t parts, units, ml, acc, bytes;  // offsets
+    int64_t leaders, parts, units, ml, acc, bytes;  // offsets
     int32_t wanted_shared, wanted_own, slots;
     int64_t max_units;
 };
@@ -616,7 +1122,8 @@ bool lay_out(int32_t max_pages, int32_t batch, int32_t num_groups, int32_t num_q
     if (w->max_units * num_kv_heads > INT32_MAX / 2)
         return false;
     auto round = [](int64_t n) { return (n + 255) / 256 * 256; };
-    w->parts = 256;
+    w->leaders = 256;
+    w->parts = w->leaders + round((int64_t)num_groups * (int64_t)sizeof(int32_t));
     w->units = w->parts + round((int64_t)batch * (int64_t)sizeof(int2));
     w->ml = w->units + round(w->max_units * (int64_t)sizeof(Unit));
     const int64_t partials = (int64_t)batch * num_q_heads * w->slots;
@@ -624,6 +1131,10 @@ bool lay_out(int32_t max_pages, int32_t batch, int32_t num_groups, int32_t num_q
     w->bytes = w->acc + round(partials * kHeadDim * (int64_t)sizeof(float));
     return true;
 }
+
+// Fewer output rows than this are merged by a work-group each: a call of few rows cuts
+// their keys into many splits, and its merge is bound by walking them.
+constexpr int kSpreadRows = 2048;
 
 // Work-groups that the device holds at once.
 constexpr int kResident = 256 * 2;
@@ -701,7 +1212,8 @@ rl_da_status rl_prefix_attn(const void* q, const void* k_pool, const void* v_poo
     a.out = (uint16_t*)out;
     a.dev_error = device_error;
     char* ws = (char*)workspace;
-    a.num_units = (int32_t*)ws;
+    a.queue = (Queue*)ws;
+    a.leaders = (int32_t*)(ws + w.leaders);
     a.parts = (int2*)(ws + w.parts);
     a.units = (Unit*)(ws + w.units);
     a.ml = (float2*)(ws + w.ml);
@@ -720,9 +1232,13 @@ rl_da_status rl_prefix_attn(const void* q, const void* k_pool, const void* v_poo
     a.slots = w.slots;
     a.wanted_shared = w.wanted_shared;
     a.wanted_own = w.wanted_own;
-    a.scale_log2 = scale * kLog2e;
+    a.scale_log2 = fabsf(scale) * kLog2e;
+    a.q_sign = scale < 0.0f ? 0x80008000u : 0u;
     hipStream_t st = (hipStream_t)stream;
-    hipLaunchKernelGGL(plan_prefix, dim3(1), dim3(kPlanThreads), 0, st, a);
+    if (batch <= kPlanSequences && num_groups <= kPlanGroups)
+        hipLaunchKernelGGL(plan_prefix<true>, dim3(1), dim3(kPlanThreads), 0, st, a);
+    else
+        hipLaunchKernelGGL(plan_prefix<false>, dim3(1), dim3(kPlanThreads), 0, st, a);
     if (hipGetLastError() != hipSuccess)
         return RL_DA_ERR_HIP;
     const int64_t most = w.max_units * num_kv_heads;
@@ -734,8 +1250,13 @@ rl_da_status rl_prefix_attn(const void* q, const void* k_pool, const void* v_poo
     if (hipGetLastError() != hipSuccess)
         return RL_DA_ERR_HIP;
     const int64_t rows = (int64_t)batch * num_q_heads;
-    hipLaunchKernelGGL(merge_prefix, dim3((unsigned)((rows + kMergeRows - 1) / kMergeRows)),
-                       dim3(kMergeRows * 32), 0, st, a);
+    if (rows < kSpreadRows)
+        hipLaunchKernelGGL(merge_prefix<true>, dim3((unsigned)rows), dim3(kMergeThreads), 0, st,
+                           a);
+    else
+        hipLaunchKernelGGL(merge_prefix<false>,
+                           dim3((unsigned)((rows + kMergeTeams - 1) / kMergeTeams)),
+                           dim3(kMergeThreads), 0, st, a);
     return hipGetLastError() == hipSuccess ? RL_DA_OK : RL_DA_ERR_HIP;
 }
 
