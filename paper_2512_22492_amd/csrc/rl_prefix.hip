@@ -30,7 +30,8 @@ namespace {
 
 constexpr int kMaxSplitPages = kWave * kUnitWaves;  // a lane of each wavefront per page
 constexpr int kMinSplitPages = 16;
-constexpr int kTargetUnits = 1024;
+constexpr int kTargetShared = 512;
+constexpr int kTargetOwn = 1024;
 constexpr int kTileRows = 128;        // query rows of a shared unit at most
 constexpr float kNoScore = -3.0e38f;  // running max before the first key
 
@@ -38,18 +39,21 @@ constexpr float kNoScore = -3.0e38f;  // running max before the first key
 // kMinSplitPages and more as many as `wanted`, what the call's shape needs to fill
 // the device.  Depends on the run's own length and the call's sizes only.
 struct Splits {
-    int count, pages;  // splits, pages of each but the last
+    int count, pages, more;  // splits; pages of each, and one more of the first `more`
+    __device__ __forceinline__ int first(int i) const { return i * pages + min(i, more); }
+    __device__ __forceinline__ int size(int i) const { return pages + (i < more ? 1 : 0); }
 };
-__host__ __device__ __forceinline__ Splits splits_of(int pages, int wanted)
+__device__ __forceinline__ Splits splits_of(int pages, int wanted)
 {
-    Splits s = {0, 0};
-    if (pages <= 0)
-        return s;
-    int n = (pages + kMaxSplitPages - 1) / kMaxSplitPages;
-    const int more = min(pages / kMinSplitPages, wanted);
-    n = more > n ? more : n;
-    s.pages = (pages + n - 1) / n;
-    s.count = (pages + s.pages - 1) / s.pages;
+    Splits s;
+    s.count = max((pages + kMaxSplitPages - 1) / kMaxSplitPages,
+                  min(pages / kMinSplitPages, wanted));
+    s.pages = pages;
+    s.more = 0;
+    if (s.count > 1) {
+        s.pages = pages / s.count;
+        s.more = pages - s.pages * s.count;
+    }
     return s;
 }
 
@@ -61,7 +65,7 @@ struct Unit {
     int32_t pages;
     int32_t limit;  // keys of the table row from here on are masked
     int32_t row0;
-    int32_t rows;
+    int32_t rows;   // negated: other units read the same pages
     int32_t slot;   // partial result's place in the row's list; -1: the row's only one
     int32_t need;   // rows of sequences shorter than this are left out
 };
@@ -188,7 +192,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_prefix(PrefixArgs a)
         o.len = length_of(b);
         o.first = g >= 0 ? shared_pages(g) : 0;
         o.shared = splits_of(o.first, a.wanted_shared).count;
-        o.s = splits_of((o.len + kPageSize - 1) / kPageSize - o.first, a.wanted_own);
+        o.s = splits_of(max((o.len + kPageSize - 1) / kPageSize - o.first, 0), a.wanted_own);
         return o;
     };
     struct Shared {
@@ -207,12 +211,12 @@ __global__ __launch_bounds__(kPlanThreads) void plan_prefix(PrefixArgs a)
 
     // Count.  A group's first member lends its table row to the shared units; a
     // group without one has none.
-    int my_group = -1;  // of the thread's first sequence
+    Own mine = {};  // the thread's first sequence
     for (int b = t; b < a.batch; b += kPlanThreads) {
         const int g = group_of(b, length_of(b));
-        if (b == t)
-            my_group = g;
         const Own o = own_of(b, g);
+        if (b == t)
+            mine = o;
         a.parts[b] = make_int2(o.shared, o.s.count);
         if (o.s.count > 0)
             atomicAdd(&cursor[length_class(o.s.pages)], o.s.count);
@@ -253,36 +257,35 @@ __global__ __launch_bounds__(kPlanThreads) void plan_prefix(PrefixArgs a)
     for (int b0 = wave * kWave; b0 < a.batch; b0 += kPlanThreads) {
         const int b = b0 + lane;
         const bool has = b < a.batch;
-        const int g = !has ? -1 : (b == t ? my_group : group_of(b, length_of(b)));
-        Own o = own_of(has ? b : b0, g);
+        Own o = mine;
+        if (b0 >= kPlanThreads)
+            o = own_of(has ? b : b0, has ? group_of(b, length_of(b)) : -1);
         o.s.count = has ? o.s.count : 0;
         int at = 0;
         if (o.s.count > 0)
             at = atomicAdd(&cursor[length_class(o.s.pages)], o.s.count);
-        auto put_own = [&](int b, int first, int pages, int len, int shared, int count, int at,
-                           int i) {
+        auto put_own = [&](int b, int first, const Splits& s, int len, int shared, int at, int i) {
             Unit u;
             u.table_row = b;
-            u.page0 = first + i * pages;
-            u.pages = min(pages, (len + kPageSize - 1) / kPageSize - u.page0);
+            u.page0 = first + s.first(i);
+            u.pages = s.size(i);
             u.limit = len;
             u.row0 = b << a.group_shift;
             u.rows = 1 << a.group_shift;
-            u.slot = shared + count == 1 ? -1 : shared + i;
+            u.slot = shared + s.count == 1 ? -1 : shared + i;
             u.need = 0;
             put(at + i, u);
         };
         // a lane writes its sequence's first units, all lanes together the others
         constexpr int kAlone = 4;
         for (int i = 0; i < min(o.s.count, kAlone); ++i)
-            put_own(b, o.first, o.s.pages, o.len, o.shared, o.s.count, at, i);
+            put_own(b, o.first, o.s, o.len, o.shared, at, i);
         for (uint64_t more = __ballot(o.s.count > kAlone); more != 0; more &= more - 1) {
             const int from = __builtin_ctzll(more);
             auto of = [&](int v) { return __builtin_amdgcn_readlane(v, from); };
-            const int count = of(o.s.count);
-            for (int i = kAlone + lane; i < count; i += kWave)
-                put_own(b0 + from, of(o.first), of(o.s.pages), of(o.len), of(o.shared), count,
-                        of(at), i);
+            const Splits s = {of(o.s.count), of(o.s.pages), of(o.s.more)};
+            for (int i = kAlone + lane; i < s.count; i += kWave)
+                put_own(b0 + from, of(o.first), s, of(o.len), of(o.shared), of(at), i);
         }
     }
     for (int g = wave; g < a.num_groups; g += kPlanWaves) {
@@ -300,11 +303,13 @@ __global__ __launch_bounds__(kPlanThreads) void plan_prefix(PrefixArgs a)
             const int split = i / h.tiles, tile = i % h.tiles;
             Unit u;
             u.table_row = first;
-            u.page0 = split * h.s.pages;
-            u.pages = min(h.s.pages, h.pages - u.page0);
+            u.page0 = h.s.first(split);
+            u.pages = h.s.size(split);
             u.limit = h.pages * kPageSize;
             u.row0 = (h.s0 << a.group_shift) + tile * kTileRows;
             u.rows = min(kTileRows, h.rows - tile * kTileRows);
+            if (h.tiles > 1)
+                u.rows = -u.rows;
             u.slot = split;
             u.need = h.pages * kPageSize;
             put(at + i, u);
@@ -368,6 +373,20 @@ __device__ __forceinline__ uint32_t lds_address(const void* p)
     return (uint32_t)(uintptr_t)(lds_void*)p;
 }
 
+// dma16, with the non-temporal hint for bytes that no other unit reads: they would
+// only push others' out of the caches (64 prompts x 8 responses: 806 us without it,
+// 736 with; 1024 e4m3 sequences of 512..2048 tokens 498, 452).
+__device__ __forceinline__ void bring16(const uint8_t* gaddr, uint32_t lds, bool once)
+{
+    if (once)
+        asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, off nt"
+                     :
+                     : "v"(gaddr), "{m0}"(lds)
+                     : "memory");
+    else
+        dma16(gaddr, lds);
+}
+
 // Eight e4m3 codes to eight bf16 (exact), in order.
 __device__ __forceinline__ uint4 widen8(uint32_t a, uint32_t b)
 {
@@ -429,7 +448,7 @@ __device__ __forceinline__ float4* join_chunk(char* tiles, int wave, int row, in
 
 template <int RB, bool FP8>
 __device__ __forceinline__ void attend_apart(const PrefixArgs& a, const Unit& u, int kvh,
-                                             AttendLds& lds, const Lanes& at)
+                                             bool once, AttendLds& lds, const Lanes& at)
 {
     const int wave = at.wave, lane = at.lane, i16 = at.i16, g4 = at.g4;
     char* const mine = lds.tiles + wave * kWaveLds;
@@ -473,8 +492,8 @@ __device__ __forceinline__ void attend_apart(const PrefixArgs& a, const Unit& u,
             const int chunk = (lane % kLanes) ^ (FP8 ? row >> 1 : chunk_swizzle(row));
             // a key past the end is read as the last one (finite, weight 0)
             const int64_t off = base + (int64_t)min(row, last) * a.row_bytes + 16 * chunk;
-            dma16(a.k_pool + off, to + 1024 * r);
-            dma16(a.v_pool + off, to + kTile + 1024 * r);
+            bring16(a.k_pool + off, to + 1024 * r, once);
+            bring16(a.v_pool + off, to + kTile + 1024 * r, once);
         }
     };
 
@@ -669,7 +688,7 @@ __device__ __forceinline__ void attend_apart(const PrefixArgs& a, const Unit& u,
 // KW wavefronts share 32 rows, each taking 1 / KW of a stage's keys.
 template <int KW, bool FP8>
 __device__ __forceinline__ void attend_together(const PrefixArgs& a, const Unit& u, int kvh,
-                                                AttendLds& lds, const Lanes& at)
+                                                bool once, AttendLds& lds, const Lanes& at)
 {
     constexpr int RB = 2;
     constexpr int KB = kStagePages / KW;  // 16-key blocks of a stage per wavefront
@@ -710,8 +729,8 @@ __device__ __forceinline__ void attend_together(const PrefixArgs& a, const Unit&
         for (int r = 0; r < kStagePages; ++r) {
             const int64_t off =
                 (int64_t)__builtin_amdgcn_readfirstlane(page[r]) * a.page_bytes + d_off;
-            dma16(a.k_pool + off, k_at + r * kPageLds + 1024 * wave);
-            dma16(a.v_pool + off, v_at + r * kPageLds + 1024 * wave);
+            bring16(a.k_pool + off, k_at + r * kPageLds + 1024 * wave, once);
+            bring16(a.v_pool + off, v_at + r * kPageLds + 1024 * wave, once);
         }
     };
     // e4m3: thread t loads the codes of dims 16 (t % 8) .. + 15 of key rows 2 (t / 8)
@@ -725,8 +744,10 @@ __device__ __forceinline__ void attend_together(const PrefixArgs& a, const Unit&
             (int64_t)lds.pages[stage * kStagePages + s_row / kPageSize] * a.page_bytes + s_off;
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            kr[i] = *reinterpret_cast<const uint4*>(a.k_pool + off + i * a.row_bytes);
-            vr[i] = *reinterpret_cast<const uint4*>(a.v_pool + off + i * a.row_bytes);
+            const uint8_t* k = a.k_pool + off + i * a.row_bytes;
+            const uint8_t* v = a.v_pool + off + i * a.row_bytes;
+            kr[i] = once ? load_stream16(k) : *reinterpret_cast<const uint4*>(k);
+            vr[i] = once ? load_stream16(v) : *reinterpret_cast<const uint4*>(v);
         }
     };
     auto stash = [&](int sel) {
@@ -991,16 +1012,18 @@ attend_prefix(PrefixArgs a)
         int taken = 0;
         if (threadIdx.x == 0)
             taken = atomicAdd(&a.queue->next, 1);
-        const Unit u = a.units[at / a.num_kv_heads];
+        Unit u = a.units[at / a.num_kv_heads];
         const int kvh = at % a.num_kv_heads;
+        const bool once = u.rows > 0;
+        u.rows = once ? u.rows : -u.rows;
         if (u.rows <= 16)
-            attend_apart<1, FP8>(a, u, kvh, lds, lanes);
+            attend_apart<1, FP8>(a, u, kvh, once, lds, lanes);
         else if (u.rows <= 32)
-            attend_apart<2, FP8>(a, u, kvh, lds, lanes);
+            attend_apart<2, FP8>(a, u, kvh, once, lds, lanes);
         else if (u.rows <= 64)
-            attend_together<2, FP8>(a, u, kvh, lds, lanes);
+            attend_together<2, FP8>(a, u, kvh, once, lds, lanes);
         else
-            attend_together<1, FP8>(a, u, kvh, lds, lanes);
+            attend_together<1, FP8>(a, u, kvh, once, lds, lanes);
         if (threadIdx.x == 0)
             lds.next_unit = gridDim.x + taken;
         __syncthreads();  // the next unit's loads overwrite what this one still read
@@ -1088,9 +1111,9 @@ struct Workspace {
     int64_t max_units;
 };
 
-int wanted_splits(int64_t pairs)
+int wanted_splits(int64_t target, int64_t pairs)
 {
-    return (int)((kTargetUnits + pairs - 1) / pairs);
+    return (int)((target + pairs - 1) / (pairs > 0 ? pairs : 1));
 }
 
 // false: sizes past what the kernels index
@@ -1103,11 +1126,11 @@ bool lay_out(int32_t max_pages, int32_t batch, int32_t num_groups, int32_t num_q
         return false;
     const int64_t tiles = (rows + kTileRows - 1) / kTileRows + num_groups;
     const int64_t pairs = (int64_t)batch * num_kv_heads;
-    w->wanted_own = wanted_splits(pairs > 0 ? pairs : 1);
+    w->wanted_own = wanted_splits(kTargetOwn, pairs);
     // a group's rows share the splits of its prefix among 128-row tiles at least
     const int64_t shared_pairs =
         (int64_t)num_kv_heads * (num_groups > rows / 128 ? num_groups : rows / 128);
-    w->wanted_shared = wanted_splits(shared_pairs > 0 ? shared_pairs : 1);
+    w->wanted_shared = wanted_splits(kTargetShared, shared_pairs);
     // splits_of takes at most pages / kMaxSplitPages + 1 or `wanted`, whichever is more
     const int32_t least = max_pages / kMaxSplitPages + 1;
     const int32_t most = max_pages / kMinSplitPages + 1;
