@@ -29,9 +29,13 @@ namespace {
 // finished sequence (length 0) takes part in nothing.
 
 constexpr int kMaxSplitPages = kWave * kUnitWaves;  // a lane of each wavefront per page
-constexpr int kMinSplitPages = 16;
+constexpr int kMinSplitPages = 32;
 constexpr int kTargetShared = 512;
 constexpr int kTargetOwn = 1024;
+// Own runs of up to a page per wavefront of a unit are a wavefront's alone: it has no one
+// to wait for, and a work-group takes four (512 sequences x 8 kv heads of one token 36 -> 19 us,
+// of 64 45 -> 38; at 256 tokens the pages of a unit's four wavefronts overlap better).
+constexpr int kAlonePages = kUnitWaves;
 constexpr int kTileRows = 128;        // query rows of a shared unit at most
 constexpr float kNoScore = -3.0e38f;  // running max before the first key
 
@@ -70,9 +74,19 @@ struct Unit {
     int32_t need;   // rows of sequences shorter than this are left out
 };
 
+// What the plan hands to the attention kernel.  Work-group g runs on XCD g % 8 and takes
+// the work at places p = g mod 8 of the list, so each XCD has a counter in a cache line
+// of its own: one counter for all of them moved between the XCDs' L2 caches at every
+// turn, about 12 ns each (4096 single-page units: 60 us with it, 19 us with eight).
+constexpr int kXcds = 8;
 struct Queue {
     int32_t units;  // of the plan, each for num_kv_heads kv heads
-    int32_t next;   // first one that no work-group has taken
+    int32_t alone;  // units that a wavefront takes by itself, behind them
+    int32_t pad[30];
+    struct {
+        int32_t next;  // places of the XCD that its work-groups have asked for
+        int32_t pad[31];
+    } xcd[kXcds];
 };
 
 struct PrefixArgs {
@@ -136,7 +150,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_prefix(PrefixArgs a)
     __shared__ int starts_lds[CACHED ? kPlanGroups + 1 : 1];
     __shared__ int pages_lds[CACHED ? kPlanGroups : 1];
     __shared__ int leader_lds[CACHED ? kPlanGroups : 1];
-    __shared__ int cursor[kClasses];
+    __shared__ int cursor[2 * kClasses];  // units by length; those for one wavefront
     const int t = threadIdx.x, lane = t % kWave, wave = t / kWave;
     const int32_t* const lens = CACHED ? lens_lds : a.seq_lens;
     const int32_t* const starts = CACHED ? starts_lds : a.group_start;
@@ -159,7 +173,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_prefix(PrefixArgs a)
     }
     if (CACHED && t == 0 && a.num_groups > 0)
         starts_lds[a.num_groups] = a.group_start[a.num_groups];
-    if (t < kClasses)
+    if (t < 2 * kClasses)
         cursor[t] = 0;
     if (long_ones && a.dev_error != nullptr)
         atomicOr(a.dev_error, RL_DA_DEVERR_LENGTH_TOO_LONG);
@@ -195,6 +209,10 @@ __global__ __launch_bounds__(kPlanThreads) void plan_prefix(PrefixArgs a)
         o.s = splits_of(max((o.len + kPageSize - 1) / kPageSize - o.first, 0), a.wanted_own);
         return o;
     };
+    auto own_class = [&](const Splits& s) {
+        const bool alone = s.count == 1 && s.pages <= kAlonePages;
+        return (alone ? kClasses : 0) + length_class(alone ? s.pages * kUnitWaves : s.pages);
+    };
     struct Shared {
         int s0, rows, tiles, pages;
         Splits s;
@@ -219,7 +237,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_prefix(PrefixArgs a)
             mine = o;
         a.parts[b] = make_int2(o.shared, o.s.count);
         if (o.s.count > 0)
-            atomicAdd(&cursor[length_class(o.s.pages)], o.s.count);
+            atomicAdd(&cursor[own_class(o.s)], o.s.count);
         if (g >= 0)
             atomicMin(&leader[g], b);
     }
@@ -232,20 +250,24 @@ __global__ __launch_bounds__(kPlanThreads) void plan_prefix(PrefixArgs a)
             atomicAdd(&cursor[length_class(h.s.pages)], h.s.count * h.tiles);
     }
     __syncthreads();
-    if (t < kClasses) {
-        int at = 0;
-        for (int c = 0; c < kClasses; ++c) {
+    if (t < 2 * kClasses) {
+        int at = 0, units = 0, all = 0;
+        for (int c = 0; c < 2 * kClasses; ++c) {
             const int n = cursor[c];
             at += c < t ? n : 0;
+            units += c < kClasses ? n : 0;
+            all += n;
         }
-        const int n = cursor[t];
         __builtin_amdgcn_wave_barrier();
         cursor[t] = at;
-        // group_start that runs backwards could name more units than there is room for
-        if (t == kClasses - 1) {
-            a.queue->units = min(at + n, a.max_units);
-            a.queue->next = 0;
+        if (t == 0) {
+            // group_start that runs backwards could name more than there is room for
+            units = min(units, a.max_units);
+            a.queue->units = units;
+            a.queue->alone = min(all, a.max_units) - units;
         }
+        if (t < kXcds)
+            a.queue->xcd[t].next = 0;
     }
     __syncthreads();
 
@@ -263,7 +285,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_prefix(PrefixArgs a)
         o.s.count = has ? o.s.count : 0;
         int at = 0;
         if (o.s.count > 0)
-            at = atomicAdd(&cursor[length_class(o.s.pages)], o.s.count);
+            at = atomicAdd(&cursor[own_class(o.s)], o.s.count);
         auto put_own = [&](int b, int first, const Splits& s, int len, int shared, int at, int i) {
             Unit u;
             u.table_row = b;
@@ -446,9 +468,12 @@ __device__ __forceinline__ float4* join_chunk(char* tiles, int wave, int row, in
            (c ^ (row & 15));
 }
 
-template <int RB, bool FP8>
-__device__ __forceinline__ void attend_apart(const PrefixArgs& a, const Unit& u, int kvh,
-                                             bool once, AttendLds& lds, const Lanes& at)
+// One wavefront's pages of a unit, u.page0 + first, + first + STEP, ..., for all of the
+// unit's rows: m, l (the lane's own keys' share) and O^T.
+template <int RB, int STEP, bool FP8>
+__device__ __forceinline__ void walk_pages(const PrefixArgs& a, const Unit& u, int kvh, int first,
+                                           bool once, AttendLds& lds, const Lanes& at,
+                                           float (&m)[RB], float (&l)[RB], floatx4_t (&o)[RB][8])
 {
     const int wave = at.wave, lane = at.lane, i16 = at.i16, g4 = at.g4;
     char* const mine = lds.tiles + wave * kWaveLds;
@@ -458,12 +483,12 @@ __device__ __forceinline__ void attend_apart(const PrefixArgs& a, const Unit& u,
     constexpr int kLoads = 2 * kTile / 1024;
     // e4m3: a page's values widened to bf16, behind the buffers of raw pages
     char* const wide = mine + kBuffers * 2 * kTile;
-    const int count = wave < u.pages ? (u.pages - wave + kUnitWaves - 1) / kUnitWaves : 0;
+    const int count = first < u.pages ? (u.pages - first + STEP - 1) / STEP : 0;
     int my_page = 0;
     float my_ks = 1.0f, my_vs = 1.0f;
     if (lane < count) {
         my_page = checked_page(a, a.block_table[(int64_t)u.table_row * a.max_pages + u.page0 +
-                                                wave + lane * kUnitWaves]);
+                                                first + lane * STEP]);
         if (FP8) {
             const int64_t slab = (int64_t)my_page * a.num_kv_heads + kvh;
             my_ks = a.k_scale[slab];
@@ -477,7 +502,7 @@ __device__ __forceinline__ void attend_apart(const PrefixArgs& a, const Unit& u,
 
     // keys of the wavefront's i-th page that count
     auto keys_of = [&](int i) {
-        return u.limit - (u.page0 + wave + i * kUnitWaves) * kPageSize;
+        return u.limit - (u.page0 + first + i * STEP) * kPageSize;
     };
     auto issue = [&](int i) {
         const int64_t page = __builtin_amdgcn_readlane(my_page, i);
@@ -497,8 +522,6 @@ __device__ __forceinline__ void attend_apart(const PrefixArgs& a, const Unit& u,
         }
     };
 
-    float m[RB], l[RB];
-    floatx4_t o[RB][8];
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
         m[rb] = kNoScore;
@@ -627,6 +650,16 @@ __device__ __forceinline__ void attend_apart(const PrefixArgs& a, const Unit& u,
         if (i + 2 < count)
             issue(i + 2);
     }
+}
+
+template <int RB, bool FP8>
+__device__ __forceinline__ void attend_apart(const PrefixArgs& a, const Unit& u, int kvh,
+                                             bool once, AttendLds& lds, const Lanes& at)
+{
+    const int wave = at.wave, i16 = at.i16, g4 = at.g4;
+    float m[RB], l[RB];
+    floatx4_t o[RB][8];
+    walk_pages<RB, kUnitWaves, FP8>(a, u, kvh, wave, once, lds, at, m, l, o);
     __syncthreads();  // all wavefronts are done with their buffers
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
@@ -683,6 +716,36 @@ __device__ __forceinline__ void attend_apart(const PrefixArgs& a, const Unit& u,
         if (u.slot >= 0 && threadIdx.x % 16 == 0)
             a.ml[part] = make_float2(M, L);
     }
+}
+
+// A whole short own run by one wavefront.
+template <bool FP8>
+__device__ __forceinline__ void attend_alone(const PrefixArgs& a, const Unit& u, int kvh,
+                                             AttendLds& lds, const Lanes& at)
+{
+    float m[1], l[1];
+    floatx4_t o[1][8];
+    walk_pages<1, 1, FP8>(a, u, kvh, 0, true, lds, at, m, l, o);
+    const float sum = sum_lanes_xor32(sum_lanes_xor16(l[0]));
+    if (at.i16 >= u.rows)
+        return;
+    const int64_t out_row = output_row(a, kvh, u.row0 + at.i16);
+    if (u.slot < 0) {
+        const float inv = 1.0f / sum;
+#pragma unroll
+        for (int db = 0; db < 8; ++db)
+            *reinterpret_cast<uint2*>(a.out + out_row * kHeadDim + 16 * db + 4 * at.g4) =
+                make_uint2(pack_bf16x2(o[0][db][0] * inv, o[0][db][1] * inv),
+                           pack_bf16x2(o[0][db][2] * inv, o[0][db][3] * inv));
+        return;
+    }
+    const int64_t part = out_row * a.slots + u.slot;
+#pragma unroll
+    for (int db = 0; db < 8; ++db)
+        *reinterpret_cast<float4*>(a.acc + part * kHeadDim + 16 * db + 4 * at.g4) =
+            make_float4(o[0][db][0], o[0][db][1], o[0][db][2], o[0][db][3]);
+    if (at.g4 == 0)
+        a.ml[part] = make_float2(m[0], sum);
 }
 
 // KW wavefronts share 32 rows, each taking 1 / KW of a stage's keys.
@@ -993,6 +1056,38 @@ __device__ __forceinline__ void attend_together(const PrefixArgs& a, const Unit&
     }
 }
 
+constexpr int kStealRounds = 3;
+
+// The place in the list of the `taken`-th one that XCD xcd's work-groups asked for (the grid
+// has taken whole rounds of XCDs before it); when its places have run out, one of the
+// XCD's that has most left (they finish up to some percent apart: 64 prompts x 8
+// responses 741 us without this, 728 with); `total` when none is left.
+__device__ __forceinline__ int next_place(const PrefixArgs& a, int total, int xcd, int taken)
+{
+    int place = gridDim.x + taken * kXcds + xcd;
+    // few rounds: the look at the others' counters, 1.5 us, would not pay
+    if (total <= kStealRounds * (int)gridDim.x)
+        return min(place, total);
+    while (place >= total) {
+        int most = 0;
+#pragma unroll
+        for (int x = 0; x < kXcds; ++x) {
+            const int left = total - x - (int)gridDim.x -
+                             kXcds * __hip_atomic_load(&a.queue->xcd[x].next, __ATOMIC_RELAXED,
+                                                       __HIP_MEMORY_SCOPE_AGENT);
+            if (left > most) {
+                most = left;
+                xcd = x;
+            }
+        }
+        if (most <= 0)
+            return total;
+        // others may be faster; every turn of this loop takes a place that is gone then
+        place = gridDim.x + atomicAdd(&a.queue->xcd[xcd].next, 1) * kXcds + xcd;
+    }
+    return place;
+}
+
 template <bool FP8>
 __global__ __launch_bounds__(kAttendThreads) __attribute__((amdgpu_waves_per_eu(2))) void
 attend_prefix(PrefixArgs a)
@@ -1003,29 +1098,39 @@ attend_prefix(PrefixArgs a)
     lanes.lane = threadIdx.x % kWave;
     lanes.i16 = lanes.lane & 15;
     lanes.g4 = lanes.lane >> 4;
-    const int total = a.queue->units * a.num_kv_heads;
+    const int units = a.queue->units * a.num_kv_heads;
+    const int alone = a.queue->alone * a.num_kv_heads;
+    const int total = units + (alone + kUnitWaves - 1) / kUnitWaves;
 
-    // A work-group's first unit is its own place in the list, the others come from the
-    // queue, asked for while the one before runs.
+    // A work-group's first work is its own place in the list, the others come from its
+    // XCD's counter, asked for while the one before runs.
+    const int xcd = blockIdx.x % kXcds;
     int at = blockIdx.x;
     while (at < total) {
         int taken = 0;
+        if (threadIdx.x == 0 && total > (int)gridDim.x)
+            taken = atomicAdd(&a.queue->xcd[xcd].next, 1);
+        if (at < units) {
+            Unit u = a.units[at / a.num_kv_heads];
+            const int kvh = at % a.num_kv_heads;
+            const bool once = u.rows > 0;
+            u.rows = once ? u.rows : -u.rows;
+            if (u.rows <= 16)
+                attend_apart<1, FP8>(a, u, kvh, once, lds, lanes);
+            else if (u.rows <= 32)
+                attend_apart<2, FP8>(a, u, kvh, once, lds, lanes);
+            else if (u.rows <= 64)
+                attend_together<2, FP8>(a, u, kvh, once, lds, lanes);
+            else
+                attend_together<1, FP8>(a, u, kvh, once, lds, lanes);
+        } else {
+            const int item = (at - units) * kUnitWaves + lanes.wave;
+            if (item < alone)
+                attend_alone<FP8>(a, a.units[a.queue->units + item / a.num_kv_heads],
+                                  item % a.num_kv_heads, lds, lanes);
+        }
         if (threadIdx.x == 0)
-            taken = atomicAdd(&a.queue->next, 1);
-        Unit u = a.units[at / a.num_kv_heads];
-        const int kvh = at % a.num_kv_heads;
-        const bool once = u.rows > 0;
-        u.rows = once ? u.rows : -u.rows;
-        if (u.rows <= 16)
-            attend_apart<1, FP8>(a, u, kvh, once, lds, lanes);
-        else if (u.rows <= 32)
-            attend_apart<2, FP8>(a, u, kvh, once, lds, lanes);
-        else if (u.rows <= 64)
-            attend_together<2, FP8>(a, u, kvh, once, lds, lanes);
-        else
-            attend_together<1, FP8>(a, u, kvh, once, lds, lanes);
-        if (threadIdx.x == 0)
-            lds.next_unit = gridDim.x + taken;
+            lds.next_unit = next_place(a, total, xcd, taken);
         __syncthreads();  // the next unit's loads overwrite what this one still read
         at = __builtin_amdgcn_readfirstlane(lds.next_unit);
     }
@@ -1145,7 +1250,7 @@ bool lay_out(int32_t max_pages, int32_t batch, int32_t num_groups, int32_t num_q
     if (w->max_units * num_kv_heads > INT32_MAX / 2)
         return false;
     auto round = [](int64_t n) { return (n + 255) / 256 * 256; };
-    w->leaders = 256;
+    w->leaders = round((int64_t)sizeof(Queue));
     w->parts = w->leaders + round((int64_t)num_groups * (int64_t)sizeof(int32_t));
     w->units = w->parts + round((int64_t)batch * (int64_t)sizeof(int2));
     w->ml = w->units + round(w->max_units * (int64_t)sizeof(Unit));
@@ -1265,7 +1370,7 @@ rl_da_status rl_prefix_attn(const void* q, const void* k_pool, const void* v_poo
     if (hipGetLastError() != hipSuccess)
         return RL_DA_ERR_HIP;
     const int64_t most = w.max_units * num_kv_heads;
-    const dim3 grid((unsigned)(most < kResident ? most : kResident));
+    const dim3 grid((unsigned)(most < kResident ? (most + kXcds - 1) / kXcds * kXcds : kResident));
     if (fp8)
         hipLaunchKernelGGL(attend_prefix<true>, grid, dim3(kAttendThreads), 0, st, a);
     else
