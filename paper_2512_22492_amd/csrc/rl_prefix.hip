@@ -798,7 +798,8 @@ __device__ __forceinline__ void attend_together(const PrefixArgs& a, const Unit&
     };
     // e4m3: thread t loads the codes of dims 16 (t % 8) .. + 15 of key rows 2 (t / 8)
     // and the next one, and widens them on the way into the tiles.
-    const int s_row = 2 * (threadIdx.x / 8), s_chunk = 2 * (threadIdx.x % 8);
+    const int thread = wave * kWave + lane;
+    const int s_row = 2 * (thread / 8), s_chunk = 2 * (thread % 8);
     const int64_t s_off = (int64_t)kvh * a.head_bytes +
                           (int64_t)(s_row % kPageSize) * a.row_bytes + 8 * s_chunk;
     uint4 kr[2], vr[2];
@@ -869,19 +870,29 @@ __device__ __forceinline__ void attend_together(const PrefixArgs& a, const Unit&
 #pragma unroll
             for (int rb = 0; rb < RB; ++rb)
                 s[rb][kb] = floatx4_t{0.0f, 0.0f, 0.0f, 0.0f};
+        // Scores, a quarter of the dims at a time; its keys are read ahead of the matrix
+        // instructions of the quarter before.
+        auto keys = [&](int ks, uint4 (&kv)[KB]) {
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb)
+                kv[kb] = *reinterpret_cast<const uint4*>(kt + kb * kPageLds + k_off[ks]);
+        };
         __builtin_amdgcn_s_setprio(1);
+        uint4 kv[2][KB];
+        keys(0, kv[0]);
 #pragma unroll
-        for (int ks = 0; ks < 4; ++ks)
+        for (int ks = 0; ks < 4; ++ks) {
+            if (ks + 1 < 4)
+                keys(ks + 1, kv[(ks + 1) % 2]);
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int kb = 0; kb < KB; ++kb) {
-                const uint4 kv =
-                    *reinterpret_cast<const uint4*>(kt + kb * kPageLds + k_off[ks]);
+            for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
                 for (int rb = 0; rb < RB; ++rb)
                     s[rb][kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                        __builtin_bit_cast(bf16x8_t, kv), __builtin_bit_cast(bf16x8_t, q[rb][ks]),
-                        s[rb][kb], 0, 0, 0);
-            }
+                        __builtin_bit_cast(bf16x8_t, kv[ks % 2][kb]),
+                        __builtin_bit_cast(bf16x8_t, q[rb][ks]), s[rb][kb], 0, 0, 0);
+        }
         __builtin_amdgcn_s_setprio(0);
         if constexpr (!FP8) {
             if (j + 1 < stages)
@@ -900,11 +911,28 @@ __device__ __forceinline__ void attend_together(const PrefixArgs& a, const Unit&
                 vs[kb] = sc.y;
             }
         }
+        // The row maxima: each block's multiplier times its raw maximum, if none of the
+        // multipliers is negative; else the scores are multiplied out first.
+        if (FP8) {
+            bool folds = true;
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb)
+                folds &= mult[kb] >= 0.0f;
+            if (__builtin_expect(!__builtin_amdgcn_readfirstlane(folds), 0)) {
+#pragma unroll
+                for (int kb = 0; kb < KB; ++kb) {
+#pragma unroll
+                    for (int rb = 0; rb < RB; ++rb)
+                        s[rb][kb] *= mult[kb];
+                    mult[kb] = 1.0f;
+                }
+            }
+        }
         float mx[RB];
         bool grow = false;
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) {
-            mx[rb] = -INFINITY;
+            float top[KB];
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb) {
                 if (kLast && page0 + kb >= u.pages) {
@@ -912,18 +940,17 @@ __device__ __forceinline__ void attend_together(const PrefixArgs& a, const Unit&
                     for (int i = 0; i < 4; ++i)
                         s[rb][kb][i] = -INFINITY;
                     mult[kb] = 1.0f;
-                    continue;
                 }
-                if (FP8) {  // multipliers of any sign
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        s[rb][kb][i] *= mult[kb];
-                }
-                const float top = __builtin_elementwise_maximum(
-                    __builtin_elementwise_maximum(s[rb][kb][0], s[rb][kb][1]),
-                    __builtin_elementwise_maximum(s[rb][kb][2], s[rb][kb][3]));
-                mx[rb] = __builtin_elementwise_maximum(mx[rb], top);
+                const float t = __builtin_elementwise_maximum(
+                    __builtin_elementwise_maximum(s[rb][kb][0], s[rb][kb][1]), s[rb][kb][2]);
+                top[kb] = __builtin_elementwise_maximum(t, s[rb][kb][3]);
+                if (FP8)
+                    top[kb] *= mult[kb];
             }
+            mx[rb] = __builtin_elementwise_maximum(top[0], top[1]);
+            if (KB == 4)
+                mx[rb] = __builtin_elementwise_maximum(
+                    __builtin_elementwise_maximum(mx[rb], top[2]), top[KB - 1]);
             if (!FP8)
                 mx[rb] *= a.scale_log2;
             mx[rb] = max_lanes_xor32(max_lanes_xor16(mx[rb]));
@@ -942,55 +969,58 @@ __device__ __forceinline__ void attend_together(const PrefixArgs& a, const Unit&
                     o[rb][db] *= alpha;
             }
         }
-        // two 16-key blocks' weights are one operand: keys 4 g4 .. + 3 of each
-        uint4 pt[RB][KB / 2];
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb)
-#pragma unroll
-            for (int kh = 0; kh < KB / 2; ++kh) {
-                uint32_t w[4];
-#pragma unroll
-                for (int half = 0; half < 4; ++half) {
-                    const int kb = 2 * kh + half / 2, i = 2 * (half % 2);
-                    float p0, p1;
-                    if (FP8) {
-                        p0 = exp2_fast(s[rb][kb][i] - m[rb]);
-                        p1 = exp2_fast(s[rb][kb][i + 1] - m[rb]);
-                        l[rb] += p0 + p1;
-                        p0 *= vs[kb];
-                        p1 *= vs[kb];
-                    } else {
-                        p0 = exp2_fast(fmaf(s[rb][kb][i], mult[kb], -m[rb]));
-                        p1 = exp2_fast(fmaf(s[rb][kb][i + 1], mult[kb], -m[rb]));
-                    }
-                    w[half] = pack_bf16x2(p0, p1);
-                }
-                pt[rb][kh] = make_uint4(w[0], w[1], w[2], w[3]);
+        // Weights as operands: two 16-key blocks (a half) are one, keys 4 g4 .. + 3 of
+        // each.  Piece i of half kh: row block i / 4, key block i / 2 % 2, key pair i % 2.
+        uint32_t pt[RB][KB / 2][4];
+        auto make_piece = [&](int kh, int i) {
+            const int rb = i / 4, kb = 2 * kh + i / 2 % 2, e = 2 * (i % 2);
+            float p0 = exp2_fast(fmaf(s[rb][kb][e], mult[kb], -m[rb]));
+            float p1 = exp2_fast(fmaf(s[rb][kb][e + 1], mult[kb], -m[rb]));
+            if (FP8) {
+                l[rb] += p0 + p1;
+                p0 *= vs[kb];
+                p1 *= vs[kb];
             }
+            pt[rb][kh][i % 4] = pack_bf16x2(p0, p1);
+        };
+        auto operand = [&](int rb, int kh) {
+            return __builtin_bit_cast(bf16x8_t, make_uint4(pt[rb][kh][0], pt[rb][kh][1],
+                                                           pt[rb][kh][2], pt[rb][kh][3]));
+        };
+#pragma unroll
+        for (int i = 0; i < 4 * RB; ++i)
+            make_piece(0, i);
+        // The value product, one dim block of a half per step; the next step's values are
+        // read ahead of this one's matrix instructions, and the second half's weights
+        // are made a piece per step of the first.
+        auto values = [&](int step) {
+            const char* p = vt + 2 * (step / 8) * kPageLds + v_off[step % 8];
+            const uint2 va = lds_read_transposed(reinterpret_cast<const uint16_t*>(p));
+            const uint2 vb = lds_read_transposed(reinterpret_cast<const uint16_t*>(p + kPageLds));
+            return __builtin_bit_cast(bf16x8_t, make_uint4(va.x, va.y, vb.x, vb.y));
+        };
         __builtin_amdgcn_s_setprio(1);
+        bf16x8_t next = values(0);
 #pragma unroll
-        for (int kh = 0; kh < KB / 2; ++kh)
+        for (int step = 0; step < 4 * KB; ++step) {
+            const bf16x8_t v = next;
+            if (step + 1 < 4 * KB)
+                next = values(step + 1);
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int db = 0; db < 8; ++db) {
-                const char* p = vt + 2 * kh * kPageLds + v_off[db];
-                const uint2 va = lds_read_transposed(reinterpret_cast<const uint16_t*>(p));
-                const uint2 vb =
-                    lds_read_transposed(reinterpret_cast<const uint16_t*>(p + kPageLds));
-                const uint4 v = make_uint4(va.x, va.y, vb.x, vb.y);
-#pragma unroll
-                for (int rb = 0; rb < RB; ++rb)
-                    o[rb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                        __builtin_bit_cast(bf16x8_t, v), __builtin_bit_cast(bf16x8_t, pt[rb][kh]),
-                        o[rb][db], 0, 0, 0);
-            }
+            for (int rb = 0; rb < RB; ++rb)
+                o[rb][step % 8] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                    v, operand(rb, step / 8), o[rb][step % 8], 0, 0, 0);
+            if (KB == 4 && step < 8)
+                make_piece(KB / 2 - 1, step);
+        }
         if (!FP8) {
 #pragma unroll
             for (int kh = 0; kh < KB / 2; ++kh)
 #pragma unroll
                 for (int rb = 0; rb < RB; ++rb)
                     lacc[rb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                        __builtin_bit_cast(bf16x8_t, ones),
-                        __builtin_bit_cast(bf16x8_t, pt[rb][kh]), lacc[rb], 0, 0, 0);
+                        __builtin_bit_cast(bf16x8_t, ones), operand(rb, kh), lacc[rb], 0, 0, 0);
         }
         __builtin_amdgcn_s_setprio(0);
     };
@@ -1093,11 +1123,7 @@ __global__ __launch_bounds__(kAttendThreads) __attribute__((amdgpu_waves_per_eu(
 attend_prefix(PrefixArgs a)
 {
     __shared__ AttendLds lds;
-    Lanes lanes;
-    lanes.wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    lanes.lane = threadIdx.x % kWave;
-    lanes.i16 = lanes.lane & 15;
-    lanes.g4 = lanes.lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int units = a.queue->units * a.num_kv_heads;
     const int alone = a.queue->alone * a.num_kv_heads;
     const int total = units + (alone + kUnitWaves - 1) / kUnitWaves;
@@ -1107,6 +1133,14 @@ attend_prefix(PrefixArgs a)
     const int xcd = blockIdx.x % kXcds;
     int at = blockIdx.x;
     while (at < total) {
+        // made anew for each unit: what a unit derives from them would otherwise be kept
+        // in registers throughout, for all four ways
+        Lanes lanes;
+        lanes.lane = threadIdx.x % kWave;
+        asm volatile("" : "+v"(lanes.lane));
+        lanes.wave = wave;
+        lanes.i16 = lanes.lane & 15;
+        lanes.g4 = lanes.lane >> 4;
         int taken = 0;
         if (threadIdx.x == 0 && total > (int)gridDim.x)
             taken = atomicAdd(&a.queue->xcd[xcd].next, 1);

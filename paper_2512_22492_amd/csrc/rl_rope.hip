@@ -4,6 +4,7 @@
 #include <type_traits>
 
 #include "rl_e4m3.h"
+#include "rl_tile.h"
 
 using namespace rl_da;
 
@@ -29,6 +30,7 @@ constexpr int kRopeThreads = 256;
 constexpr int kRopeRows = kRopeThreads / kRowLanes;  // rows in flight per work-group
 constexpr int kLaneDims = kHeadDim / kRowLanes;
 static_assert(kRopeRows == kPageSize, "a work-group's rows are the slots of a page");
+constexpr int kAhead = 6;  // head rows that a thread of rope_append_pages has in flight
 constexpr int kDppRowRor8 = 0x128;
 
 struct RopeArgs {
@@ -137,23 +139,22 @@ __device__ __forceinline__ void turn_row(const RopeArgs& a, const uint16_t* norm
         for (int i = 0; i < kLaneDims; ++i)
             x[i] = x[i] * r * w[i];
     }
-    float other[kLaneDims];
-    if (INTERLEAVED) {
+    if (!INTERLEAVED && a.rotary_dim == kHeadDim) {
 #pragma unroll
-        for (int i = 0; i < kLaneDims; ++i)
-            other[i] = x[i ^ 1];
-    } else if (a.rotary_dim == kHeadDim) {
-#pragma unroll
-        for (int i = 0; i < kLaneDims; ++i)
-            other[i] = dpp_f32<kDppRowRor8>(x[i]);
-    } else {
-        const int step = a.rotary_dim / 2 / kLaneDims;
-        const int from = kLaneDims * j >= a.rotary_dim ? j : (j < step ? j + step : j - step);
-#pragma unroll
-        for (int i = 0; i < kLaneDims; ++i)
-            other[i] = __shfl(x[i], from, kRowLanes);
+        for (int i = 0; i < kLaneDims; ++i) {
+            const float other = __int_as_float(__builtin_amdgcn_update_dpp(
+                0, __float_as_int(x[i]), kDppRowRor8, 0xf, 0xf, true));
+            x[i] = fmaf(x[i], t.c[i], other * t.s[i]);
+        }
+        return;
     }
-    // a row past rotary_dim keeps its value, whatever its partner holds
+    float other[kLaneDims];
+    const int step = a.rotary_dim / 2 / kLaneDims;
+    const int from = j < step ? j + step : j - step;
+#pragma unroll
+    for (int i = 0; i < kLaneDims; ++i)
+        other[i] = INTERLEAVED ? x[i ^ 1] : __shfl(x[i], from & (kRowLanes - 1), kRowLanes);
+    // a lane past rotary_dim keeps its values, whatever its partner holds
     if (kLaneDims * j < a.rotary_dim) {
 #pragma unroll
         for (int i = 0; i < kLaneDims; ++i)
@@ -167,6 +168,13 @@ __device__ __forceinline__ uint4 pack8(const float (&x)[kLaneDims])
                       pack_bf16x2(x[6], x[7]));
 }
 
+// A store with the non-temporal hint: the queries of a prompt are more than the caches
+// hold until they are read (50k tokens: 257 us without the hints, 246 with).
+__device__ __forceinline__ void store_stream16(uint16_t* p, const uint4& v)
+{
+    __builtin_nontemporal_store(u32x4_t{v.x, v.y, v.z, v.w}, reinterpret_cast<u32x4_t*>(p));
+}
+
 __device__ __forceinline__ float absmax8(const float (&x)[kLaneDims])
 {
     float m = 0.0f;
@@ -176,12 +184,32 @@ __device__ __forceinline__ float absmax8(const float (&x)[kLaneDims])
     return m;
 }
 
+// Quotients by one divisor d, rounded as a / d is: with r = 1 / d rounded to nearest and
+// q = a r, q + (a - q d) r is the correctly rounded quotient (P. Markstein,
+// "Computation of elementary functions on the IBM RISC System/6000 processor", IBM J.
+// Res. Dev. 34, 1990), three operations an element, as long as nothing leaves the
+// normal range: kScaleLow <= d <= kScaleHigh keeps every a that an e4m3 code tells
+// from zero, and its remainder, far inside it.
+constexpr float kScaleLow = 0x1p-60f, kScaleHigh = 0x1p60f;
+
+// A row at its slab's scale.  The scale is at least absmax / 448 rounded, so that an
+// element exceeds 448 by a rounding at most, which e4m3's rounding removes; scales so
+// small that their own rounding is coarse take the division and the clamp.
 __device__ __forceinline__ uint2 encode8(const float (&x)[kLaneDims], float scale)
 {
     float y[kLaneDims];
+    if (scale >= kScaleLow && scale <= kScaleHigh) {
+        const float r = 1.0f / scale;
 #pragma unroll
-    for (int i = 0; i < kLaneDims; ++i)
-        y[i] = clamp448(x[i] / scale);
+        for (int i = 0; i < kLaneDims; ++i) {
+            const float q = x[i] * r;
+            y[i] = fmaf(fmaf(-q, scale, x[i]), r, q);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < kLaneDims; ++i)
+            y[i] = clamp448(x[i] / scale);
+    }
     return make_uint2(e4m3_pair(y[0], y[1]) | (e4m3_pair(y[2], y[3]) << 16),
                       e4m3_pair(y[4], y[5]) | (e4m3_pair(y[6], y[7]) << 16));
 }
@@ -308,7 +336,7 @@ __global__ __launch_bounds__(kRopeThreads) void rope_append_token(RopeArgs a)
 template <bool FP8, bool INTERLEAVED>
 __global__ __launch_bounds__(kRopeThreads) void rope_append_pages(RopeArgs a)
 {
-    __shared__ float top[2][kRopeThreads / kWave];
+    __shared__ float top[2][kAhead][kRopeThreads / kWave];
     const int part = blockIdx.x % a.parts;
     const int tile = (int)(blockIdx.x / a.parts) % a.tiles;
     const int b = (int)(blockIdx.x / a.parts) / a.tiles;
@@ -340,63 +368,97 @@ __global__ __launch_bounds__(kRopeThreads) void rope_append_pages(RopeArgs a)
     const bool live = pos >= L && pos < min(end, cap);
     const int64_t token = token0 + (live ? pos - L : 0);
     const int held = tile == 0 ? L % kPageSize : 0;  // slots of earlier tokens
+    const int64_t row_at = page * a.page_bytes + (int64_t)slot * a.row_bytes;
     Turn t;
     float wq[kLaneDims], wk[kLaneDims];
     load_turn<INTERLEAVED>(a, live ? pos : 0, j, t);
     load_weight(a.q_norm, j, wq);
     load_weight(a.k_norm, j, wk);
 
+    // kAhead head rows are read side by side (50k prompt tokens of 48 head rows, bf16 and
+    // e4m3: four 245 and 349 us, six 241 and 244, eight 246 and 282; one at a time and
+    // without the parts 296 and 310), and an e4m3 round's slabs share a barrier.
     const int heads = a.num_q_heads + 2 * a.num_kv_heads;
+    const int first_kv = a.num_q_heads;
     int round = 0;
-    for (int at = part; at < heads; at += a.parts, ++round) {
-        const HeadRow r = head_row(a, at);
-        float x[kLaneDims];
-        uint4 bits = make_uint4(0, 0, 0, 0);
-        if (live)
-            bits = *reinterpret_cast<const uint4*>(row_source(a, r, token) + kLaneDims * j);
-        unpack8(bits, x);
-        if (r.is_q)
-            turn_row<INTERLEAVED>(a, a.q_norm, wq, t, j, x);
-        else if (!r.is_v)
-            turn_row<INTERLEAVED>(a, a.k_norm, wk, t, j, x);
-        if (r.is_q) {
-            if (live)
-                *reinterpret_cast<uint4*>(a.q_out + (token * a.num_q_heads + r.head) * kHeadDim +
-                                          kLaneDims * j) = pack8(x);
-            continue;
-        }
-        uint8_t* row = (r.is_v ? a.v_pool : a.k_pool) + page * a.page_bytes +
-                       (int64_t)r.head * a.head_bytes + (int64_t)slot * a.row_bytes;
-        if (!FP8) {
-            if (live)
-                *reinterpret_cast<uint4*>(row + 16 * j) = r.is_v ? bits : pack8(x);
-            continue;
-        }
-        // the largest magnitude of the slab's new tokens (idle rows hold zeros,
-        // whose norm is zero as well)
-        float m = row16_max(live ? absmax8(x) : 0.0f);
-        m = fmaxf(m, __shfl_xor(m, 16));
-        m = fmaxf(m, __shfl_xor(m, 32));
-        if (threadIdx.x % kWave == 0)
-            top[round & 1][threadIdx.x / kWave] = m;
-        float* scale =
-            (r.is_v ? a.v_scale : a.k_scale) + (int64_t)page * a.num_kv_heads + r.head;
-        const float was = *scale;
-        __syncthreads();  // the scale is read by all rows before one of them writes it
+    for (int at0 = part * kAhead; at0 < heads; at0 += a.parts * kAhead, ++round) {
+        uint4 bits[kAhead];
+        float was[kAhead];
 #pragma unroll
-        for (int w = 0; w < kRopeThreads / kWave; ++w)
-            m = fmaxf(m, top[round & 1][w]);
-        const float now = joined_scale(m, held > 0, was);
-        if (live) {
-            *reinterpret_cast<uint2*>(row + 8 * j) = encode8(x, now);
-        } else if (slot < held && now != was) {
-            uint2* c = reinterpret_cast<uint2*>(row + 8 * j);
-            *c = shrink8(*c, was / now);
+        for (int i = 0; i < kAhead; ++i) {
+            const HeadRow r = head_row(a, min(at0 + i, heads - 1));
+            bits[i] = make_uint4(0, 0, 0, 0);
+            if (live)
+                bits[i] = load_stream16(
+                    reinterpret_cast<const uint8_t*>(row_source(a, r, token) + kLaneDims * j));
+            was[i] = 1.0f;
+            if (FP8 && !r.is_q)
+                was[i] = (r.is_v ? a.v_scale : a.k_scale)[(int64_t)page * a.num_kv_heads + r.head];
         }
-        if (threadIdx.x == 0)
-            *scale = now;
+        float x[kAhead][kLaneDims];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            if (at0 + i >= heads)
+                break;
+            const HeadRow r = head_row(a, at0 + i);
+            unpack8(bits[i], x[i]);
+            if (r.is_q)
+                turn_row<INTERLEAVED>(a, a.q_norm, wq, t, j, x[i]);
+            else if (!r.is_v)
+                turn_row<INTERLEAVED>(a, a.k_norm, wk, t, j, x[i]);
+            if (r.is_q) {
+                if (live)
+                    store_stream16(a.q_out + (token * a.num_q_heads + r.head) * kHeadDim +
+                                       kLaneDims * j,
+                                   pack8(x[i]));
+            } else if (!FP8) {
+                if (live)
+                    *reinterpret_cast<uint4*>((r.is_v ? a.v_pool : a.k_pool) + row_at +
+                                              (int64_t)r.head * a.head_bytes + 16 * j) =
+                        r.is_v ? bits[i] : pack8(x[i]);
+            } else {
+                // the largest magnitude of the slab's new tokens (idle rows count nothing)
+                const float m = max_lanes_xor32(
+                    max_lanes_xor16(row16_max(live ? absmax8(x[i]) : 0.0f)));
+                if (threadIdx.x % kWave == 0)
+                    top[round & 1][i][threadIdx.x / kWave] = m;
+            }
+        }
+        if (!FP8 || at0 + kAhead <= first_kv)
+            continue;
+        __syncthreads();  // also: the scales are read by all rows before one writes them
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            if (at0 + i >= heads)
+                break;
+            if (at0 + i < first_kv)
+                continue;
+            const HeadRow r = head_row(a, at0 + i);
+            float m = 0.0f;
+#pragma unroll
+            for (int w = 0; w < kRopeThreads / kWave; ++w)
+                m = fmaxf(m, top[round & 1][i][w]);
+            const float now = joined_scale(m, held > 0, was[i]);
+            uint8_t* row = (r.is_v ? a.v_pool : a.k_pool) + row_at +
+                           (int64_t)r.head * a.head_bytes + 8 * j;
+            if (live) {
+                *reinterpret_cast<uint2*>(row) = encode8(x[i], now);
+            } else if (slot < held && now != was[i]) {
+                uint2* c = reinterpret_cast<uint2*>(row);
+                *c = shrink8(*c, was[i] / now);
+            }
+            if (threadIdx.x == 0)
+                (r.is_v ? a.v_scale
+                        : a.k_scale)[(int64_t)page * a.num_kv_heads + r.head] = now;
+        }
     }
 }
+
+// Work-groups that share a page's head rows: enough for a few rounds of the device (12
+// replies of 5..90 tokens 30.4 -> 12.7 us), and at least kMinParts, so that the last
+// round is short (50k prompt tokens: 284 us with one, 258 with four).
+constexpr int64_t kPageGroups = 4096;
+constexpr int64_t kMinParts = 4;
 
 }  // namespace
 
@@ -490,7 +552,11 @@ rl_da_status rl_rope_append(const void* q, int64_t q_stride, const void* k_new, 
     if (one) {
         a.parts = (int32_t)((heads + kRopeRows - 1) / kRopeRows);
     } else {
-        a.parts = 1;
+        const int64_t most = (heads + kAhead - 1) / kAhead;
+        const int64_t parts = (kPageGroups + pages - 1) / pages;
+        a.parts = (int32_t)(parts < kMinParts ? kMinParts : parts);
+        if (a.parts > most)
+            a.parts = (int32_t)most;
     }
     if (pages * a.parts > INT32_MAX)
         return RL_DA_ERR_UNSUPPORTED;
