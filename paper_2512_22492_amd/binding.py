@@ -506,28 +506,38 @@ def _device_index(device):
     return torch.cuda.current_device() if device.index is None else device.index
 
 
-def _on_device(index, call):
-    """call() with the GPU `index` current, where the library launches."""
+def _on_device(index, fn, *args):
+    """fn(*args) with the GPU `index` current, where the library launches."""
     import torch
     if torch.cuda.current_device() == index:
-        return call()
+        return fn(*args)
     with torch.cuda.device(index):
-        return call()
+        return fn(*args)
 
 
-def _token_stride(name, t, heads, head_dim, dtype, device, tokens=None):
-    """The token stride of head rows [T, heads, head_dim] that are contiguous within a
-    token (a slice of a fused projection's heads, say); raises ValueError else."""
-    _check_tensor(name, t, dtype=dtype, shape=(tokens, heads, head_dim), device=device,
-                  contiguous=False)
+def _token_stride(name, t, shape, dtype, device):
+    """The token stride of head rows t, of `shape` (tokens, heads, head_dim), that are
+    contiguous within a token (a slice of a fused projection's heads, say); raises
+    ValueError else."""
+    tokens, heads, dim = shape
+    # on every step's path: what is as it should be takes the cheap comparisons only
+    try:
+        if t.dtype is dtype and t.shape == shape and t.device == device:
+            stride, row, one = t.stride()
+            if (one == 1 and row == dim and stride >= heads * dim and stride % 8 == 0
+                    and tokens > 1):
+                return stride
+    except AttributeError:
+        pass
+    _check_tensor(name, t, dtype=dtype, shape=shape, device=device, contiguous=False)
     if t.numel() == 0 or t.is_contiguous():
-        return heads * head_dim
+        return heads * dim
     stride, row, one = t.stride()
-    if one != 1 or (heads > 1 and row != head_dim):
+    if one != 1 or (heads > 1 and row != dim):
         raise ValueError("%s must have contiguous head rows, has strides %s" % (name, t.stride()))
-    if t.shape[0] == 1:
-        return heads * head_dim
-    if stride < heads * head_dim or stride % 8:
+    if tokens == 1:
+        return heads * dim
+    if stride < heads * dim or stride % 8:
         raise ValueError("%s must have a token stride that is a multiple of 8 and holds its "
                          "heads, has %d" % (name, stride))
     return stride
@@ -545,8 +555,9 @@ class RopeAppender:
         import torch
         dt = RL_DA_KV_BF16 if p.kv_dtype == "bf16" else RL_DA_KV_FP8_E4M3
         dev = self.device = p.k_pool.device
-        self.batch, self.head_dim = p.batch, p.head_dim
-        self.num_q_heads, self.num_kv_heads = p.num_q_heads, p.num_kv_heads
+        self.batch = p.batch
+        self._rows = (torch.bfloat16, dev, (p.num_q_heads, p.head_dim),
+                      (p.num_kv_heads, p.head_dim))
         _check_pools(p.k_pool, p.v_pool, p.k_scale, p.v_scale, kv_dtype=dt,
                      layout=LAYOUTS[p.layout], num_kv_heads=p.num_kv_heads,
                      head_dim=p.head_dim, page_size=p.page_size, device=dev)
@@ -577,24 +588,24 @@ class RopeAppender:
         and v_new [T, Hkv, D] (bf16) from positions seq_lens on: one token per sequence,
         or with q_start [B + 1] rows q_start[b] .. q_start[b + 1] - 1 of sequence b, at
         most max_q_per_seq of them; raises on a bad status."""
-        import torch
-        dev, bf16, D = self.device, torch.bfloat16, self.head_dim
-        tokens = self.batch if q_start is None else None
+        bf16, dev, q_rows, kv_rows = self._rows
+        tokens = self.batch
         if q_start is not None:
-            _check_tensor("q_start", q_start, dtype=torch.int32, shape=(self.batch + 1,),
-                          device=dev)
-            tokens = int(q.shape[0]) if hasattr(q, "shape") and len(q.shape) else None
-        qs = _token_stride("q", q, self.num_q_heads, D, bf16, dev, tokens)
-        ks = _token_stride("k_new", k_new, self.num_kv_heads, D, bf16, dev, tokens)
-        vs = _token_stride("v_new", v_new, self.num_kv_heads, D, bf16, dev, tokens)
-        _check_tensor("q_out", q_out, dtype=bf16, shape=(tokens, self.num_q_heads, D),
-                      device=dev)
+            import torch
+            _check_tensor("q_start", q_start, dtype=torch.int32, shape=(tokens + 1,), device=dev)
+            _check_tensor("q", q, ndim=3, contiguous=False)
+            tokens = int(q.shape[0])
+        q_shape, kv_shape = (tokens,) + q_rows, (tokens,) + kv_rows
+        qs = _token_stride("q", q, q_shape, bf16, dev)
+        ks = _token_stride("k_new", k_new, kv_shape, bf16, dev)
+        vs = _token_stride("v_new", v_new, kv_shape, bf16, dev)
+        if _token_stride("q_out", q_out, q_shape, bf16, dev) != q_rows[0] * q_rows[1]:
+            raise ValueError("q_out must be contiguous")
         if tokens == 0:
             return
-        rc = _on_device(self._index, lambda: self._fn(
-            q.data_ptr(), qs, k_new.data_ptr(), ks, v_new.data_ptr(), vs, _ptr(q_start),
-            int(max_q_per_seq), *self._turn_args, q_out.data_ptr(), *self._cache_args,
-            _stream(stream)))
+        rc = _on_device(self._index, self._fn, q.data_ptr(), qs, k_new.data_ptr(), ks,
+                        v_new.data_ptr(), vs, _ptr(q_start), max_q_per_seq, *self._turn_args,
+                        q_out.data_ptr(), *self._cache_args, _stream(stream))
         if rc != RL_DA_OK:
             raise RLDecodeAttnError(rc, "rl_rope_append")
 
@@ -709,8 +720,8 @@ class PrefixAttention:
         _check_tensor("out", out, dtype=torch.bfloat16, shape=self.want, device=self.device)
         if self._streams is not None:
             self._note_stream(stream)
-        rc = _on_device(self._index, lambda: self._fn(
-            q.data_ptr(), *self._before, out.data_ptr(), *self._behind, _stream(stream)))
+        rc = _on_device(self._index, self._fn, q.data_ptr(), *self._before, out.data_ptr(),
+                        *self._behind, _stream(stream))
         if rc != RL_DA_OK:
             raise RLDecodeAttnError(rc, "rl_prefix_attn")
 

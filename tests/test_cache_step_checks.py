@@ -127,7 +127,7 @@ def test_binding_checks_prefix_tensors(monkeypatch):
         with pytest.raises(ValueError, match="group_start|prefix_pages"):
             B.PrefixAttention(p, s, n)
     monkeypatch.setattr(B, "_device_index", lambda d: 0)
-    monkeypatch.setattr(B, "_on_device", lambda i, call: call())
+    monkeypatch.setattr(B, "_on_device", lambda i, fn, *args: fn(*args))
     need = B.rl_prefix_attn_workspace_size(4, 3, 1, 4, 2)[1]
     ws = torch.zeros(need, dtype=torch.uint8)
     for bad in (ws[:-1], ws[::2], ws.view(torch.int32), ws.view(2, -1), 7):
@@ -161,7 +161,7 @@ def test_binding_checks_rope_tensors(monkeypatch):
         with pytest.raises(ValueError, match="cos_sin|norm|device_error"):
             B.RopeAppender(p, **{**dict(cos_sin=cs), **kw})
     monkeypatch.setattr(B, "_device_index", lambda d: 0)
-    monkeypatch.setattr(B, "_on_device", lambda i, call: call())
+    monkeypatch.setattr(B, "_on_device", lambda i, fn, *args: fn(*args))
     app = B.RopeAppender(p, cs, q_norm=w, k_norm=w)
     seen = []
     app._fn = lambda *a: seen.append(a) or OK
