@@ -138,11 +138,87 @@ __device__ __forceinline__ int length_class(int pages)
     return kClasses - 1 - min((pages - 1) / (kMaxSplitPages / kClasses), kClasses - 1);
 }
 
+// A unit that all lanes hold alike, in scalar registers.
+__device__ __forceinline__ Unit scalar_unit(const Unit& u)
+{
+    auto s = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+    return {s(u.table_row), s(u.page0), s(u.pages), s(u.limit),
+            s(u.row0),      s(u.rows),  s(u.slot),  s(u.need)};
+}
+
+// A sequence's own run and its splits.
+struct Own {
+    int len, first, shared;  // tokens, first own page, partial results of the shared ones
+    Splits s;
+    __device__ __forceinline__ bool alone() const { return s.count == 1 && s.pages <= kAlonePages; }
+};
+__device__ __forceinline__ Own own_of(const PrefixArgs& a, int len, int shared_pages)
+{
+    Own o;
+    o.len = len;
+    o.first = shared_pages;
+    o.shared = splits_of(o.first, a.wanted_shared).count;
+    o.s = splits_of(max((o.len + kPageSize - 1) / kPageSize - o.first, 0), a.wanted_own);
+    return o;
+}
+__device__ __forceinline__ Unit own_unit(const PrefixArgs& a, int b, const Own& o, int i)
+{
+    Unit u;
+    u.table_row = b;
+    u.page0 = o.first + o.s.first(i);
+    u.pages = o.s.size(i);
+    u.limit = o.len;
+    u.row0 = b << a.group_shift;
+    u.rows = 1 << a.group_shift;
+    u.slot = o.shared + o.s.count == 1 ? -1 : o.shared + i;
+    u.need = 0;
+    return u;
+}
+
+// A group's shared run: its splits, each for every tile of query rows.
+struct Shared {
+    int s0, rows, tiles, pages;
+    Splits s;
+    __device__ __forceinline__ int units() const { return s.count * tiles; }
+};
+__device__ __forceinline__ int shared_pages(const PrefixArgs& a, int pages)
+{
+    return max(0, min(pages, a.max_pages));
+}
+__device__ __forceinline__ Shared shared_of(const PrefixArgs& a, int start, int end, int pages)
+{
+    Shared h;
+    h.s0 = max(0, min(start, a.batch));
+    h.rows = (max(h.s0, min(end, a.batch)) - h.s0) << a.group_shift;
+    h.tiles = (h.rows + kTileRows - 1) / kTileRows;
+    h.pages = shared_pages(a, pages);
+    h.s = splits_of(h.pages, a.wanted_shared);
+    return h;
+}
+// Unit i of a group; a split's tiles follow each other: they read the same pages, from
+// the table row of `leader`, a member.
+__device__ __forceinline__ Unit shared_unit(const PrefixArgs& a, const Shared& h, int leader, int i)
+{
+    const int split = i / h.tiles, tile = i % h.tiles;
+    Unit u;
+    u.table_row = leader;
+    u.page0 = h.s.first(split);
+    u.pages = h.s.size(split);
+    u.limit = h.pages * kPageSize;
+    u.row0 = (h.s0 << a.group_shift) + tile * kTileRows;
+    u.rows = min(kTileRows, h.rows - tile * kTileRows);
+    if (h.tiles > 1)
+        u.rows = -u.rows;
+    u.slot = split;
+    u.need = h.pages * kPageSize;
+    return u;
+}
+
 // Writes the units, longest first, and each sequence's number of partial results.
 // Units of one class stand in any order: where a unit's results go does not depend
 // on it.  One work-group, bound by the latency of what it reads: lengths and groups
 // are read once, side by side, and everything after that is LDS (512 sequences in 64
-// groups: 9.4 us).
+// groups: 7 us).
 template <bool CACHED>
 __global__ __launch_bounds__(kPlanThreads) void plan_prefix(PrefixArgs a)
 {
@@ -179,8 +255,6 @@ __global__ __launch_bounds__(kPlanThreads) void plan_prefix(PrefixArgs a)
         atomicOr(a.dev_error, RL_DA_DEVERR_LENGTH_TOO_LONG);
     __syncthreads();
     auto length_of = [&](int b) { return max(0, min(lens[b], cap)); };
-    auto shared_pages = [&](int g) { return max(0, min(pages[g], a.max_pages)); };
-
     // The group that a sequence is a member of (it fills the group's shared pages),
     // or -1.
     auto group_of = [&](int b, int len) {
@@ -194,37 +268,21 @@ __global__ __launch_bounds__(kPlanThreads) void plan_prefix(PrefixArgs a)
         }
         if (lo < 0 || starts[lo + 1] <= b)
             return -1;
-        const int p = shared_pages(lo);
+        const int p = shared_pages(a, pages[lo]);
         return p > 0 && len >= p * kPageSize ? lo : -1;
     };
-    struct Own {
-        int len, first, shared;  // first own page, splits of the shared ones
-        Splits s;
+    auto own_at = [&](int b, int g) {
+        return own_of(a, length_of(b), g >= 0 ? shared_pages(a, pages[g]) : 0);
     };
-    auto own_of = [&](int b, int g) {
-        Own o;
-        o.len = length_of(b);
-        o.first = g >= 0 ? shared_pages(g) : 0;
-        o.shared = splits_of(o.first, a.wanted_shared).count;
-        o.s = splits_of(max((o.len + kPageSize - 1) / kPageSize - o.first, 0), a.wanted_own);
-        return o;
+    auto own_class = [&](const Own& o) {
+        return o.alone() ? kClasses + length_class(o.s.pages * kUnitWaves)
+                         : length_class(o.s.pages);
     };
-    auto own_class = [&](const Splits& s) {
-        const bool alone = s.count == 1 && s.pages <= kAlonePages;
-        return (alone ? kClasses : 0) + length_class(alone ? s.pages * kUnitWaves : s.pages);
-    };
-    struct Shared {
-        int s0, rows, tiles, pages;
-        Splits s;
-    };
-    auto shared_of = [&](int g) {
-        Shared h;
-        h.s0 = max(0, min(starts[g], a.batch));
-        h.rows = (max(h.s0, min(starts[g + 1], a.batch)) - h.s0) << a.group_shift;
-        h.tiles = (h.rows + kTileRows - 1) / kTileRows;
-        h.pages = shared_pages(g);
-        h.s = splits_of(h.pages, a.wanted_shared);
-        return h;
+    auto shared_at = [&](int g) { return shared_of(a, starts[g], starts[g + 1], pages[g]); };
+    // (atomics pass the first-level cache, so must what reads their results from memory)
+    auto leader_of = [&](int g) {
+        return CACHED ? leader[g]
+                      : __hip_atomic_load(&leader[g], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     };
 
     // Count.  A group's first member lends its table row to the shared units; a
@@ -232,22 +290,22 @@ __global__ __launch_bounds__(kPlanThreads) void plan_prefix(PrefixArgs a)
     Own mine = {};  // the thread's first sequence
     for (int b = t; b < a.batch; b += kPlanThreads) {
         const int g = group_of(b, length_of(b));
-        const Own o = own_of(b, g);
+        const Own o = own_at(b, g);
         if (b == t)
             mine = o;
         a.parts[b] = make_int2(o.shared, o.s.count);
         if (o.s.count > 0)
-            atomicAdd(&cursor[own_class(o.s)], o.s.count);
+            atomicAdd(&cursor[own_class(o)], o.s.count);
         if (g >= 0)
             atomicMin(&leader[g], b);
     }
     __syncthreads();
     for (int g = t; g < a.num_groups; g += kPlanThreads) {
-        if (leader[g] == INT32_MAX)
+        if (leader_of(g) == INT32_MAX)
             continue;
-        const Shared h = shared_of(g);
-        if (h.s.count * h.tiles > 0)
-            atomicAdd(&cursor[length_class(h.s.pages)], h.s.count * h.tiles);
+        const Shared h = shared_at(g);
+        if (h.units() > 0)
+            atomicAdd(&cursor[length_class(h.s.pages)], h.units());
     }
     __syncthreads();
     if (t < 2 * kClasses) {
@@ -281,62 +339,134 @@ __global__ __launch_bounds__(kPlanThreads) void plan_prefix(PrefixArgs a)
         const bool has = b < a.batch;
         Own o = mine;
         if (b0 >= kPlanThreads)
-            o = own_of(has ? b : b0, has ? group_of(b, length_of(b)) : -1);
+            o = own_at(has ? b : b0, has ? group_of(b, length_of(b)) : -1);
         o.s.count = has ? o.s.count : 0;
         int at = 0;
         if (o.s.count > 0)
-            at = atomicAdd(&cursor[own_class(o.s)], o.s.count);
-        auto put_own = [&](int b, int first, const Splits& s, int len, int shared, int at, int i) {
-            Unit u;
-            u.table_row = b;
-            u.page0 = first + s.first(i);
-            u.pages = s.size(i);
-            u.limit = len;
-            u.row0 = b << a.group_shift;
-            u.rows = 1 << a.group_shift;
-            u.slot = shared + s.count == 1 ? -1 : shared + i;
-            u.need = 0;
-            put(at + i, u);
-        };
+            at = atomicAdd(&cursor[own_class(o)], o.s.count);
         // a lane writes its sequence's first units, all lanes together the others
-        constexpr int kAlone = 4;
-        for (int i = 0; i < min(o.s.count, kAlone); ++i)
-            put_own(b, o.first, o.s, o.len, o.shared, at, i);
-        for (uint64_t more = __ballot(o.s.count > kAlone); more != 0; more &= more - 1) {
+        constexpr int kFirst = 4;
+        for (int i = 0; i < min(o.s.count, kFirst); ++i)
+            put(at + i, own_unit(a, b, o, i));
+        for (uint64_t more = __ballot(o.s.count > kFirst); more != 0; more &= more - 1) {
             const int from = __builtin_ctzll(more);
             auto of = [&](int v) { return __builtin_amdgcn_readlane(v, from); };
-            const Splits s = {of(o.s.count), of(o.s.pages), of(o.s.more)};
-            for (int i = kAlone + lane; i < s.count; i += kWave)
-                put_own(b0 + from, of(o.first), s, of(o.len), of(o.shared), of(at), i);
+            const Own w = {of(o.len), of(o.first), of(o.shared),
+                           {of(o.s.count), of(o.s.pages), of(o.s.more)}};
+            for (int i = kFirst + lane; i < w.s.count; i += kWave)
+                put(of(at) + i, own_unit(a, b0 + from, w, i));
         }
     }
     for (int g = wave; g < a.num_groups; g += kPlanWaves) {
-        const int first = leader[g];
+        const int first = leader_of(g);
         if (first == INT32_MAX)
             continue;
-        const Shared h = shared_of(g);
-        const int n = h.s.count * h.tiles;
+        const Shared h = shared_at(g);
+        const int n = h.units();
         int at = 0;
         if (lane == 0 && n > 0)
             at = atomicAdd(&cursor[length_class(h.s.pages)], n);
         at = __builtin_amdgcn_readfirstlane(at);
-        // a split's tiles follow each other: they read the same pages
-        for (int i = lane; i < n; i += kWave) {
-            const int split = i / h.tiles, tile = i % h.tiles;
-            Unit u;
-            u.table_row = first;
-            u.page0 = h.s.first(split);
-            u.pages = h.s.size(split);
-            u.limit = h.pages * kPageSize;
-            u.row0 = (h.s0 << a.group_shift) + tile * kTileRows;
-            u.rows = min(kTileRows, h.rows - tile * kTileRows);
-            if (h.tiles > 1)
-                u.rows = -u.rows;
-            u.slot = split;
-            u.need = h.pages * kPageSize;
-            put(at + i, u);
+        for (int i = lane; i < n; i += kWave)
+            put(at + i, shared_unit(a, h, first, i));
+    }
+}
+
+// The plan of a small call, which every work-group of the attention kernel makes for
+// itself, a lane per sequence and per group: the launch of plan_prefix and the wait for
+// it are %SMALL%.
+constexpr int kSmallCall = kWave;  // sequences and groups at most
+
+struct SmallPlan {
+    // running numbers of units, and what each is made from
+    int shared_end[kSmallCall], own_end[kSmallCall];
+    Shared shared[kSmallCall];
+    int leader[kSmallCall];
+    Own own[kSmallCall];
+    int alone_seq[kSmallCall];  // sequences whose own run is a wavefront's alone
+    int units, alone;
+};
+
+__device__ __forceinline__ int wave_inclusive_sum(int v, int lane)
+{
+#pragma unroll
+    for (int d = 1; d < kWave; d *= 2) {
+        const int below = __shfl_up(v, d);
+        v += lane >= d ? below : 0;
+    }
+    return v;
+}
+
+// By one wavefront; `tell`: it also writes the numbers of partial results for the merge.
+__device__ __forceinline__ void plan_small(const PrefixArgs& a, SmallPlan& plan, int lane,
+                                           bool tell)
+{
+    const bool is_seq = lane < a.batch, is_group = lane < a.num_groups;
+    const int cap = a.max_pages * kPageSize;
+    const int raw = is_seq ? a.seq_lens[lane] : 0;
+    const int start = is_group ? a.group_start[lane] : INT32_MAX;
+    const int end = is_group ? a.group_start[lane + 1] : INT32_MAX;
+    const int pages = is_group ? shared_pages(a, a.prefix_pages[lane]) : 0;
+    const int len = max(0, min(raw, cap));
+    // the last group that starts at or before the lane's sequence
+    int lo = -1, hi = a.num_groups;
+#pragma unroll
+    for (int step = kSmallCall; step > 0; step /= 2) {  // all lanes take part in the reads
+        const int mid = max((lo + hi) / 2, 0);
+        const bool below = __shfl(start, mid) <= lane;
+        if (hi - lo > 1) {
+            lo = below ? mid : lo;
+            hi = below ? hi : mid;
         }
     }
+    const int group_end = __shfl(end, max(lo, 0)), group_pages = __shfl(pages, max(lo, 0));
+    const bool member = is_seq && lo >= 0 && group_end > lane && group_pages > 0 &&
+                        len >= group_pages * kPageSize;
+    const Own o = own_of(a, len, member ? group_pages : 0);
+    const uint64_t members = __ballot(member);
+    const bool alone = o.alone();
+    const uint64_t alone_mask = __ballot(alone);
+    if (alone)
+        plan.alone_seq[__popcll(alone_mask & ((1ull << lane) - 1))] = lane;
+    plan.own[lane] = o;
+
+    const Shared h = shared_of(a, is_group ? start : 0, is_group ? end : 0, pages);
+    const int s1 = h.s0 + (h.rows >> a.group_shift);
+    const uint64_t in_group = h.rows == 0 ? 0
+                                          : (s1 < 64 ? (1ull << s1) - 1 : ~0ull) &
+                                                ~((1ull << h.s0) - 1) & members;
+    plan.shared[lane] = h;
+    plan.leader[lane] = in_group != 0 ? (int)__builtin_ctzll(in_group) : 0;
+    const int shared_end = wave_inclusive_sum(in_group != 0 ? h.units() : 0, lane);
+    const int shared_all = __builtin_amdgcn_readlane(shared_end, kWave - 1);
+    const int own_end = shared_all + wave_inclusive_sum(alone ? 0 : o.s.count, lane);
+    plan.shared_end[lane] = shared_end;
+    plan.own_end[lane] = own_end;
+    if (lane == kWave - 1) {
+        plan.units = own_end;
+        plan.alone = __popcll(alone_mask);
+    }
+    if (tell) {
+        if (is_seq)
+            a.parts[lane] = make_int2(o.shared, o.s.count);
+        if (raw > cap && a.dev_error != nullptr)
+            atomicOr(a.dev_error, RL_DA_DEVERR_LENGTH_TOO_LONG);
+    }
+}
+
+// Unit number i of a small call's plan.
+__device__ __forceinline__ Unit small_unit(const PrefixArgs& a, const SmallPlan& plan, int lane,
+                                           int i)
+{
+    const uint64_t shared = __ballot(plan.shared_end[lane] > i);
+    if (shared != 0) {
+        const int g = __builtin_ctzll(shared);
+        return shared_unit(a, plan.shared[g], plan.leader[g],
+                           i - (g > 0 ? plan.shared_end[g - 1] : 0));
+    }
+    const int b = __builtin_ctzll(__ballot(plan.own_end[lane] > i));
+    return own_unit(a, b, plan.own[b],
+                    i - (b > 0 ? plan.own_end[b - 1] : plan.shared_end[kSmallCall - 1]));
 }
 
 // ---------------------------------------------------------------- attend ---
@@ -1118,18 +1248,31 @@ __device__ __forceinline__ int next_place(const PrefixArgs& a, int total, int xc
     return place;
 }
 
-template <bool FP8>
+template <bool FP8, bool SMALL>
 __global__ __launch_bounds__(kAttendThreads) __attribute__((amdgpu_waves_per_eu(2))) void
 attend_prefix(PrefixArgs a)
 {
     __shared__ AttendLds lds;
+    __shared__ std::conditional_t<SMALL, SmallPlan, int> plan;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const int units = a.queue->units * a.num_kv_heads;
-    const int alone = a.queue->alone * a.num_kv_heads;
+    int planned, planned_alone;
+    if constexpr (SMALL) {
+        if (wave == 0)
+            plan_small(a, plan, threadIdx.x, blockIdx.x == 0);
+        __syncthreads();
+        planned = __builtin_amdgcn_readfirstlane(plan.units);
+        planned_alone = __builtin_amdgcn_readfirstlane(plan.alone);
+    } else {
+        planned = a.queue->units;
+        planned_alone = a.queue->alone;
+    }
+    const int units = planned * a.num_kv_heads;
+    const int alone = planned_alone * a.num_kv_heads;
     const int total = units + (alone + kUnitWaves - 1) / kUnitWaves;
 
     // A work-group's first work is its own place in the list, the others come from its
-    // XCD's counter, asked for while the one before runs.
+    // XCD's counter, asked for while the one before runs (a small call, of hardly more
+    // than one round, deals them out in turn).
     const int xcd = blockIdx.x % kXcds;
     int at = blockIdx.x;
     while (at < total) {
@@ -1142,10 +1285,14 @@ attend_prefix(PrefixArgs a)
         lanes.i16 = lanes.lane & 15;
         lanes.g4 = lanes.lane >> 4;
         int taken = 0;
-        if (threadIdx.x == 0 && total > (int)gridDim.x)
+        if (!SMALL && threadIdx.x == 0 && total > (int)gridDim.x)
             taken = atomicAdd(&a.queue->xcd[xcd].next, 1);
         if (at < units) {
-            Unit u = a.units[at / a.num_kv_heads];
+            Unit u;
+            if constexpr (SMALL)
+                u = scalar_unit(small_unit(a, plan, lanes.lane, at / a.num_kv_heads));
+            else
+                u = a.units[at / a.num_kv_heads];
             const int kvh = at % a.num_kv_heads;
             const bool once = u.rows > 0;
             u.rows = once ? u.rows : -u.rows;
@@ -1159,14 +1306,22 @@ attend_prefix(PrefixArgs a)
                 attend_together<1, FP8>(a, u, kvh, once, lds, lanes);
         } else {
             const int item = (at - units) * kUnitWaves + lanes.wave;
-            if (item < alone)
-                attend_alone<FP8>(a, a.units[a.queue->units + item / a.num_kv_heads],
-                                  item % a.num_kv_heads, lds, lanes);
+            if (item < alone) {
+                const int n = item / a.num_kv_heads;
+                Unit u;
+                if constexpr (SMALL) {
+                    const int b = __builtin_amdgcn_readfirstlane(plan.alone_seq[n]);
+                    u = scalar_unit(own_unit(a, b, plan.own[b], 0));
+                } else {
+                    u = a.units[planned + n];
+                }
+                attend_alone<FP8>(a, u, item % a.num_kv_heads, lds, lanes);
+            }
         }
-        if (threadIdx.x == 0)
+        if (!SMALL && threadIdx.x == 0)
             lds.next_unit = next_place(a, total, xcd, taken);
         __syncthreads();  // the next unit's loads overwrite what this one still read
-        at = __builtin_amdgcn_readfirstlane(lds.next_unit);
+        at = SMALL ? at + (int)gridDim.x : __builtin_amdgcn_readfirstlane(lds.next_unit);
     }
 }
 
@@ -1397,18 +1552,21 @@ rl_da_status rl_prefix_attn(const void* q, const void* k_pool, const void* v_poo
     a.scale_log2 = fabsf(scale) * kLog2e;
     a.q_sign = scale < 0.0f ? 0x80008000u : 0u;
     hipStream_t st = (hipStream_t)stream;
-    if (batch <= kPlanSequences && num_groups <= kPlanGroups)
-        hipLaunchKernelGGL(plan_prefix<true>, dim3(1), dim3(kPlanThreads), 0, st, a);
-    else
-        hipLaunchKernelGGL(plan_prefix<false>, dim3(1), dim3(kPlanThreads), 0, st, a);
-    if (hipGetLastError() != hipSuccess)
-        return RL_DA_ERR_HIP;
+    const bool small = batch <= kSmallCall && num_groups <= kSmallCall;
+    if (!small) {
+        if (batch <= kPlanSequences && num_groups <= kPlanGroups)
+            hipLaunchKernelGGL(plan_prefix<true>, dim3(1), dim3(kPlanThreads), 0, st, a);
+        else
+            hipLaunchKernelGGL(plan_prefix<false>, dim3(1), dim3(kPlanThreads), 0, st, a);
+        if (hipGetLastError() != hipSuccess)
+            return RL_DA_ERR_HIP;
+    }
     const int64_t most = w.max_units * num_kv_heads;
     const dim3 grid((unsigned)(most < kResident ? (most + kXcds - 1) / kXcds * kXcds : kResident));
-    if (fp8)
-        hipLaunchKernelGGL(attend_prefix<true>, grid, dim3(kAttendThreads), 0, st, a);
-    else
-        hipLaunchKernelGGL(attend_prefix<false>, grid, dim3(kAttendThreads), 0, st, a);
+    void (*attend)(PrefixArgs) = fp8 ? (small ? attend_prefix<true, true> : attend_prefix<true, false>)
+                                     : (small ? attend_prefix<false, true>
+                                              : attend_prefix<false, false>);
+    hipLaunchKernelGGL(attend, grid, dim3(kAttendThreads), 0, st, a);
     if (hipGetLastError() != hipSuccess)
         return RL_DA_ERR_HIP;
     const int64_t rows = (int64_t)batch * num_q_heads;

@@ -175,6 +175,35 @@ def test_more_sequences_and_groups_than_the_plan_has_threads():
     check(p, "2500 groups")
 
 
+@pytest.mark.parametrize("kv", ["bf16", "fp8_e4m3"])
+@pytest.mark.parametrize("batch", [1, 63, 64, 65])
+def test_small_calls_and_the_next_larger(batch, kv):
+    """Up to 64 sequences and groups a call is planned in another way than above: the
+    same groups either way, down to groups of one and sequences in none."""
+    rng = np.random.default_rng(batch)
+    sizes, left = [], batch - min(batch - 1, 3)
+    while left:
+        sizes.append(int(rng.integers(0, min(left, 9) + 1)))
+        left -= sizes[-1]
+    prefix = [int(x) for x in rng.integers(0, 40, len(sizes))]
+    lens = np.repeat(prefix, sizes) * PAGE + rng.integers(0, 700, sum(sizes))
+    behind = batch - sum(sizes)
+    lens = np.concatenate([lens, rng.integers(0, 300, behind)])
+    lens[rng.random(batch) < 0.1] = 0
+    p = problem(sizes, prefix, lens, hq=8, hkv=2, kv=kv, seed=71, behind=behind)
+    check(p, "batch %d %s" % (batch, kv))
+
+
+def test_many_groups_of_few_sequences():
+    """64 and 65 groups, most without sequences, over a batch of 40."""
+    for groups in (64, 65):
+        sizes = [1 if g % 3 == 1 else (2 if g % 7 == 0 else 0) for g in range(groups)]
+        sizes[-1] += 40 - sum(sizes)
+        prefix = [(5 * g) % 11 for g in range(groups)]
+        lens = np.repeat(prefix, sizes) * PAGE + np.arange(40) * 3
+        check(problem(sizes, prefix, lens, hq=4, hkv=1, seed=72), "%d groups" % groups)
+
+
 def test_scales_of_either_sign_and_zero():
     for scale in (0.0, -0.125, 2.0):
         p = problem([5, 3], [6, 2], [100, 96, 130, 0, 97, 32, 50, 33], seed=80, kv="bf16")
