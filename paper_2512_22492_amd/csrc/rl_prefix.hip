@@ -29,9 +29,6 @@ namespace {
 // finished sequence (length 0) takes part in nothing.
 
 constexpr int kMaxSplitPages = kWave * kUnitWaves;  // a lane of each wavefront per page
-constexpr int kMinSplitPages = 32;
-constexpr int kTargetShared = 512;
-constexpr int kTargetOwn = 1024;
 // Own runs of up to a page per wavefront of a unit are a wavefront's alone: it has no one
 // to wait for, and a work-group takes four (512 sequences x 8 kv heads of one token 36 -> 19 us,
 // of 64 45 -> 38; at 256 tokens the pages of a unit's four wavefronts overlap better).
@@ -39,19 +36,19 @@ constexpr int kAlonePages = kUnitWaves;
 constexpr int kTileRows = 128;        // query rows of a shared unit at most
 constexpr float kNoScore = -3.0e38f;  // running max before the first key
 
-// Splits of a run of `pages` pages: no longer than kMaxSplitPages, and for runs of
-// kMinSplitPages and more as many as `wanted`, what the call's shape needs to fill
-// the device.  Depends on the run's own length and the call's sizes only.
+// Splits of a run of `pages` pages: no longer than kMaxSplitPages, and as many as
+// `wanted`, what the call's shape needs to fill the device, of 2^least_shift pages at
+// least.  Depends on the run's own length and the call's sizes only.
 struct Splits {
     int count, pages, more;  // splits; pages of each, and one more of the first `more`
     __device__ __forceinline__ int first(int i) const { return i * pages + min(i, more); }
     __device__ __forceinline__ int size(int i) const { return pages + (i < more ? 1 : 0); }
 };
-__device__ __forceinline__ Splits splits_of(int pages, int wanted)
+__device__ __forceinline__ Splits splits_of(int pages, int wanted, int least_shift)
 {
     Splits s;
     s.count = max((pages + kMaxSplitPages - 1) / kMaxSplitPages,
-                  min(pages / kMinSplitPages, wanted));
+                  min(pages >> least_shift, wanted));
     s.pages = pages;
     s.more = 0;
     if (s.count > 1) {
@@ -119,8 +116,10 @@ struct PrefixArgs {
     int32_t max_pages;
     int32_t max_units;
     int32_t slots;
+    int32_t unshared_pages;     // prefixes up to this length count as own pages
     int32_t wanted_shared;      // splits that fill the device (splits_of)
     int32_t wanted_own;
+    int32_t least_shift;        // log2 of a split's least pages
     float scale_log2;           // |scale| * log2(e)
     uint32_t q_sign;            // 0x80008000 for a negative scale: Q enters negated
 };
@@ -157,8 +156,9 @@ __device__ __forceinline__ Own own_of(const PrefixArgs& a, int len, int shared_p
     Own o;
     o.len = len;
     o.first = shared_pages;
-    o.shared = splits_of(o.first, a.wanted_shared).count;
-    o.s = splits_of(max((o.len + kPageSize - 1) / kPageSize - o.first, 0), a.wanted_own);
+    o.shared = splits_of(o.first, a.wanted_shared, a.least_shift).count;
+    o.s = splits_of(max((o.len + kPageSize - 1) / kPageSize - o.first, 0), a.wanted_own,
+                    a.least_shift);
     return o;
 }
 __device__ __forceinline__ Unit own_unit(const PrefixArgs& a, int b, const Own& o, int i)
@@ -183,7 +183,8 @@ struct Shared {
 };
 __device__ __forceinline__ int shared_pages(const PrefixArgs& a, int pages)
 {
-    return max(0, min(pages, a.max_pages));
+    const int p = max(0, min(pages, a.max_pages));
+    return p > a.unshared_pages ? p : 0;
 }
 __device__ __forceinline__ Shared shared_of(const PrefixArgs& a, int start, int end, int pages)
 {
@@ -192,7 +193,7 @@ __device__ __forceinline__ Shared shared_of(const PrefixArgs& a, int start, int 
     h.rows = (max(h.s0, min(end, a.batch)) - h.s0) << a.group_shift;
     h.tiles = (h.rows + kTileRows - 1) / kTileRows;
     h.pages = shared_pages(a, pages);
-    h.s = splits_of(h.pages, a.wanted_shared);
+    h.s = splits_of(h.pages, a.wanted_shared, a.least_shift);
     return h;
 }
 // Unit i of a group; a split's tiles follow each other: they read the same pages, from
@@ -374,7 +375,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_prefix(PrefixArgs a)
 
 // The plan of a small call, which every work-group of the attention kernel makes for
 // itself, a lane per sequence and per group: the launch of plan_prefix and the wait for
-// it are %SMALL%.
+// it cost 3 us (four responses to a short prompt 15.2 -> 12.2).
 constexpr int kSmallCall = kWave;  // sequences and groups at most
 
 struct SmallPlan {
@@ -1325,6 +1326,35 @@ attend_prefix(PrefixArgs a)
     }
 }
 
+// A call whose table is narrow and whose work-groups are few: a work-group per sequence
+// and kv head attends the whole row, shared pages included, and writes the output; no
+// plan, no partial results and no merge.
+template <bool FP8>
+__global__ __launch_bounds__(kAttendThreads) void attend_rows(PrefixArgs a)
+{
+    __shared__ AttendLds lds;
+    Lanes lanes;
+    lanes.wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    lanes.lane = threadIdx.x % kWave;
+    lanes.i16 = lanes.lane & 15;
+    lanes.g4 = lanes.lane >> 4;
+    const int b = blockIdx.x / a.num_kv_heads, kvh = blockIdx.x % a.num_kv_heads;
+    const int cap = a.max_pages * kPageSize;
+    const int raw = a.seq_lens[b];
+    if (raw > cap && a.dev_error != nullptr && threadIdx.x == 0)
+        atomicOr(a.dev_error, RL_DA_DEVERR_LENGTH_TOO_LONG);
+    const int len = min(raw, cap), G = 1 << a.group_shift;
+    if (len <= 0) {  // no keys: zeros
+        uint2* out = reinterpret_cast<uint2*>(
+            a.out + ((int64_t)b * a.num_q_heads + kvh * G) * kHeadDim);
+        for (int i = threadIdx.x; i < G * kHeadDim / 4; i += kAttendThreads)
+            out[i] = make_uint2(0, 0);
+        return;
+    }
+    const Unit u = {b, 0, (len + kPageSize - 1) / kPageSize, len, b << a.group_shift, G, -1, 0};
+    attend_apart<1, FP8>(a, u, kvh, false, lds, lanes);
+}
+
 // ----------------------------------------------------------------- merge ---
 //
 // 32 lanes per output row, four dims each, walk a row's partial results in order;
@@ -1401,9 +1431,23 @@ __global__ __launch_bounds__(kMergeThreads) void merge_prefix(PrefixArgs a)
 
 struct Workspace {
     int64_t leaders, parts, units, ml, acc, bytes;  // offsets
-    int32_t wanted_shared, wanted_own, slots;
+    int32_t wanted_shared, wanted_own, least_shift, slots;
     int64_t max_units;
 };
+
+// Work-groups that the device holds at once.
+constexpr int kResident = 256 * 2;
+
+// How many units a call's shared and own runs are cut into, kv heads included, and the
+// least pages of one.  A call whose (sequence, kv head) pairs leave the device idle is
+// cut finely, into one round of units in all; one that fills it coarsely, since units
+// and their partial results cost more there (8 responses of 1000..8000 tokens to one
+// prompt of 2000, 8 kv heads: 39.5 us cut coarsely, 31.6 finely; 64 responses of 2000 to 8
+// prompts 105.5 coarsely, 114.4 finely).
+struct SplitGoal {
+    int shared, own, least_shift;
+};
+constexpr SplitGoal kFewPairs = {512, 512, 4}, kManyPairs = {512, 1024, 5};
 
 int wanted_splits(int64_t target, int64_t pairs)
 {
@@ -1420,14 +1464,16 @@ bool lay_out(int32_t max_pages, int32_t batch, int32_t num_groups, int32_t num_q
         return false;
     const int64_t tiles = (rows + kTileRows - 1) / kTileRows + num_groups;
     const int64_t pairs = (int64_t)batch * num_kv_heads;
-    w->wanted_own = wanted_splits(kTargetOwn, pairs);
+    const SplitGoal& goal = pairs < kResident ? kFewPairs : kManyPairs;
+    w->least_shift = goal.least_shift;
+    w->wanted_own = wanted_splits(goal.own, pairs);
     // a group's rows share the splits of its prefix among 128-row tiles at least
     const int64_t shared_pairs =
-        (int64_t)num_kv_heads * (num_groups > rows / 128 ? num_groups : rows / 128);
-    w->wanted_shared = wanted_splits(kTargetShared, shared_pairs);
+        (int64_t)num_kv_heads * (num_groups > rows / kTileRows ? num_groups : rows / kTileRows);
+    w->wanted_shared = wanted_splits(goal.shared, shared_pairs);
     // splits_of takes at most pages / kMaxSplitPages + 1 or `wanted`, whichever is more
     const int32_t least = max_pages / kMaxSplitPages + 1;
-    const int32_t most = max_pages / kMinSplitPages + 1;
+    const int32_t most = (max_pages >> goal.least_shift) + 1;
     const int32_t shared = least > (w->wanted_shared < most ? w->wanted_shared : most)
                                ? least
                                : (w->wanted_shared < most ? w->wanted_shared : most);
@@ -1453,8 +1499,14 @@ bool lay_out(int32_t max_pages, int32_t batch, int32_t num_groups, int32_t num_q
 // their keys into many splits, and its merge is bound by walking them.
 constexpr int kSpreadRows = 2048;
 
-// Work-groups that the device holds at once.
-constexpr int kResident = 256 * 2;
+// In calls whose (sequence, kv head) pairs fit the device at once a short prefix is read
+// with each sequence's own pages: it comes from the caches, and a unit and a partial
+// result less is worth more (16 responses of up to 80 tokens to 2 prompts of 400, 8 kv heads: 16.7 -> 13.5
+// us; 150 to 600: 19.9 -> 17.1).
+constexpr int kUnsharedPages = 48;
+// Tables up to this width are then attended row by row altogether (the same
+// calls with tables as wide as they need: 16.6 -> 9.0 us, 19.8 -> 11.8; 64 pages 23.0 -> 14.8).
+constexpr int kRowPages = 64;
 
 }  // namespace
 
@@ -1547,11 +1599,21 @@ rl_da_status rl_prefix_attn(const void* q, const void* k_pool, const void* v_poo
     a.max_pages = max_pages;
     a.max_units = (int32_t)w.max_units;
     a.slots = w.slots;
+    a.unshared_pages = (int64_t)batch * num_kv_heads <= kResident ? kUnsharedPages : 0;
     a.wanted_shared = w.wanted_shared;
     a.wanted_own = w.wanted_own;
+    a.least_shift = w.least_shift;
     a.scale_log2 = fabsf(scale) * kLog2e;
     a.q_sign = scale < 0.0f ? 0x80008000u : 0u;
     hipStream_t st = (hipStream_t)stream;
+    if (max_pages <= kRowPages && (int64_t)batch * num_kv_heads <= kResident) {
+        const dim3 grid((unsigned)(batch * num_kv_heads));
+        if (fp8)
+            hipLaunchKernelGGL(attend_rows<true>, grid, dim3(kAttendThreads), 0, st, a);
+        else
+            hipLaunchKernelGGL(attend_rows<false>, grid, dim3(kAttendThreads), 0, st, a);
+        return hipGetLastError() == hipSuccess ? RL_DA_OK : RL_DA_ERR_HIP;
+    }
     const bool small = batch <= kSmallCall && num_groups <= kSmallCall;
     if (!small) {
         if (batch <= kPlanSequences && num_groups <= kPlanGroups)
