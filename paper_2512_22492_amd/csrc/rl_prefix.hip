@@ -219,7 +219,7 @@ __device__ __forceinline__ Unit shared_unit(const PrefixArgs& a, const Shared& h
 // Units of one class stand in any order: where a unit's results go does not depend
 // on it.  One work-group, bound by the latency of what it reads: lengths and groups
 // are read once, side by side, and everything after that is LDS (512 sequences in 64
-// groups: 7 us).
+// groups: 5.5 us).
 template <bool CACHED>
 __global__ __launch_bounds__(kPlanThreads) void plan_prefix(PrefixArgs a)
 {
@@ -331,6 +331,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_prefix(PrefixArgs a)
     __syncthreads();
 
     // Write.
+    constexpr int kFirst = 4;
     auto put = [&](int at, const Unit& u) {
         if (at < a.max_units)
             a.units[at] = u;
@@ -346,7 +347,6 @@ __global__ __launch_bounds__(kPlanThreads) void plan_prefix(PrefixArgs a)
         if (o.s.count > 0)
             at = atomicAdd(&cursor[own_class(o)], o.s.count);
         // a lane writes its sequence's first units, all lanes together the others
-        constexpr int kFirst = 4;
         for (int i = 0; i < min(o.s.count, kFirst); ++i)
             put(at + i, own_unit(a, b, o, i));
         for (uint64_t more = __ballot(o.s.count > kFirst); more != 0; more &= more - 1) {
@@ -358,18 +358,26 @@ __global__ __launch_bounds__(kPlanThreads) void plan_prefix(PrefixArgs a)
                 put(of(at) + i, own_unit(a, b0 + from, w, i));
         }
     }
-    for (int g = wave; g < a.num_groups; g += kPlanWaves) {
-        const int first = leader_of(g);
-        if (first == INT32_MAX)
-            continue;
-        const Shared h = shared_at(g);
-        const int n = h.units();
+    // the groups likewise, from the last wavefront on, which has fewest sequences
+    for (int g0 = (kPlanWaves - 1 - wave) * kWave; g0 < a.num_groups; g0 += kPlanThreads) {
+        const int g = g0 + lane;
+        const bool has = g < a.num_groups;
+        const int first = has ? leader_of(g) : INT32_MAX;
+        const Shared h = shared_at(has ? g : g0);
+        const int n = first != INT32_MAX ? h.units() : 0;
         int at = 0;
-        if (lane == 0 && n > 0)
+        if (n > 0)
             at = atomicAdd(&cursor[length_class(h.s.pages)], n);
-        at = __builtin_amdgcn_readfirstlane(at);
-        for (int i = lane; i < n; i += kWave)
+        for (int i = 0; i < min(n, kFirst); ++i)
             put(at + i, shared_unit(a, h, first, i));
+        for (uint64_t more = __ballot(n > kFirst); more != 0; more &= more - 1) {
+            const int from = __builtin_ctzll(more);
+            auto of = [&](int v) { return __builtin_amdgcn_readlane(v, from); };
+            const Shared w = {of(h.s0), of(h.rows), of(h.tiles), of(h.pages),
+                              {of(h.s.count), of(h.s.pages), of(h.s.more)}};
+            for (int i = kFirst + lane; i < of(n); i += kWave)
+                put(of(at) + i, shared_unit(a, w, of(first), i));
+        }
     }
 }
 
