@@ -363,7 +363,7 @@ rl_da_status rl_kv_append(const void* k_new, const void* v_new, void* k_pool, vo
  * [0, num_pages) (RL_DA_DEVERR_PAGE_OUT_OF_RANGE): nothing of a skipped token is
  * written, its row of q_out included.  Needs no handle and no workspace; enqueues
  * one kernel on `stream`.  Any rl_da_layout; head_dim 128, page_size 16, rotary_dim
- * a multiple of 16 up to 128 only (else UNSUPPORTED); q, k_new, v_new, cos_sin, the
+ * a multiple of 16 up to 128, pages (all kv heads) under 2 GiB only (else UNSUPPORTED); q, k_new, v_new, cos_sin, the
  * norm weights, q_out and the pools 16-byte aligned.
  */
 rl_da_status rl_rope_append(const void* q, int64_t q_stride, const void* k_new, int64_t k_stride,
@@ -382,7 +382,9 @@ rl_da_status rl_rope_append(const void* q, int64_t q_stride, const void* k_new, 
  * Decode attention over shared prefixes: rl_decode_attn_run's result for a batch
  * whose sequences share their first pages in groups (the responses to one prompt,
  * 8 of each in the paper's rollouts, Sec. 7.1; a system prompt under all of them),
- * with each group's shared pages read once instead of once per sequence.
+ * with each group's shared pages read once instead of once per sequence (short
+ * prefixes of calls that leave the device idle may be read with each sequence's own
+ * pages, which is faster there).
  *   group_start   [num_groups + 1] int32, non-decreasing: group g is sequences
  *                 group_start[g] .. group_start[g + 1] - 1; sequences before the first
  *                 group and behind the last share nothing
@@ -397,8 +399,8 @@ rl_da_status rl_rope_append(const void* q, int64_t q_stride, const void* k_new, 
  * The workspace is device memory of at least rl_prefix_attn_workspace_size bytes
  * for these sizes, 16-byte aligned; the launches of this call alone write and read
  * it, so it needs no initial contents, may be reused or freed once the stream has
- * passed them, and calls that can overlap bring one each.  Enqueues three kernels on
- * `stream` and allocates nothing.  Deterministic: keys are cut where the call's sizes
+ * passed them, and calls that can overlap bring one each.  Enqueues one to three
+ * kernels on `stream` and allocates nothing.  Deterministic: keys are cut where the call's sizes
  * and the sequence's and its prefix's lengths say, and a row's partial results join
  * in a fixed order.
  *
@@ -407,8 +409,8 @@ rl_da_status rl_rope_append(const void* q, int64_t q_stride, const void* k_new, 
  * non-NULL, with RL_DA_DEVERR_PAGE_OUT_OF_RANGE, and the outputs of that sequence
  * (that group's members) are then undefined; a length beyond max_pages * page_size
  * is cut there and reported with RL_DA_DEVERR_LENGTH_TOO_LONG.  The bits are only
- * ever set.  head_dim 128, page_size 16, Hq / Hkv in {1, 2, 4, 8, 16} (else
- * UNSUPPORTED); q, the pools and out 16-byte aligned.
+ * ever set.  head_dim 128, page_size 16, Hq / Hkv in {1, 2, 4, 8, 16}, pages (all kv
+ * heads) under 2 GiB (else UNSUPPORTED); q, the pools and out 16-byte aligned.
  */
 rl_da_status rl_prefix_attn_workspace_size(int32_t max_pages, int32_t batch, int32_t num_groups,
                                            int32_t num_q_heads, int32_t num_kv_heads,

@@ -1567,7 +1567,8 @@ rl_da_status rl_prefix_attn(const void* q, const void* k_pool, const void* v_poo
         return RL_DA_ERR_INVALID_ARG;
     const int G = num_q_heads / num_kv_heads;
     if (head_dim != kHeadDim || page_size != kPageSize ||
-        (G != 1 && G != 2 && G != 4 && G != 8 && G != 16))
+        (G != 1 && G != 2 && G != 4 && G != 8 && G != 16) ||
+        ps.page >= ((int64_t)1 << 31))  // strides inside a page are 32-bit
         return RL_DA_ERR_UNSUPPORTED;
     Workspace w;
     if (!lay_out(max_pages, batch, num_groups, num_q_heads, num_kv_heads, &w))

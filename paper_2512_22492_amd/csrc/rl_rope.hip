@@ -72,8 +72,8 @@ __device__ __forceinline__ void report(const RopeArgs& a, int32_t bits)
         atomicOr(a.dev_error, bits);
 }
 
-// A lane's cosines and sines: dims 8j..8j+7 of the row.  Dims that are not
-// rotated have cosine 1 and sine 0.
+// A lane's cosines and sines: dims 8j..8j+7 of the row (of no use to lanes past
+// rotary_dim).  Loads without branches: a branch around a load waits for it at its end.
 struct Turn {
     float c[kLaneDims], s[kLaneDims];
 };
@@ -82,45 +82,25 @@ template <bool INTERLEAVED>
 __device__ __forceinline__ void load_turn(const RopeArgs& a, int pos, int j, Turn& t)
 {
     const int half = a.rotary_dim / 2;
+    const bool low = kLaneDims * j < half;
+    // dims 2i, 2i + 1 turn by angle i, or dims i, i + half
+    const int dim = kLaneDims * j < a.rotary_dim ? kLaneDims * j : 0;
+    const int at = INTERLEAVED ? dim / 2 : (dim >= half ? dim - half : dim);
+    const float* row = a.cos_sin + (int64_t)pos * a.rotary_dim + at;
+    float c[kLaneDims], s[kLaneDims];
+#pragma unroll
+    for (int v = 0; v < (INTERLEAVED ? 1 : 2); ++v) {
+        const float4 x = *reinterpret_cast<const float4*>(row + 4 * v);
+        const float4 y = *reinterpret_cast<const float4*>(row + half + 4 * v);
+        c[4 * v] = x.x, c[4 * v + 1] = x.y, c[4 * v + 2] = x.z, c[4 * v + 3] = x.w;
+        s[4 * v] = y.x, s[4 * v + 1] = y.y, s[4 * v + 2] = y.z, s[4 * v + 3] = y.w;
+    }
 #pragma unroll
     for (int i = 0; i < kLaneDims; ++i) {
-        t.c[i] = 1.0f;
-        t.s[i] = 0.0f;
+        t.c[i] = c[INTERLEAVED ? i / 2 : i];
+        const float sine = s[INTERLEAVED ? i / 2 : i];
+        t.s[i] = (INTERLEAVED ? i % 2 == 0 : low) ? -sine : sine;
     }
-    if (kLaneDims * j >= a.rotary_dim)
-        return;
-    const float* row = a.cos_sin + (int64_t)pos * a.rotary_dim;
-    if (INTERLEAVED) {  // dims 2i, 2i + 1 turn by angle i
-        const float4 c = *reinterpret_cast<const float4*>(row + 4 * j);
-        const float4 s = *reinterpret_cast<const float4*>(row + half + 4 * j);
-        const float cc[4] = {c.x, c.y, c.z, c.w}, ss[4] = {s.x, s.y, s.z, s.w};
-#pragma unroll
-        for (int i = 0; i < kLaneDims; ++i) {
-            t.c[i] = cc[i / 2];
-            t.s[i] = i % 2 ? ss[i / 2] : -ss[i / 2];
-        }
-    } else {  // dims i, i + half turn by angle i
-        const bool low = kLaneDims * j < half;
-        const int at = kLaneDims * j - (low ? 0 : half);
-#pragma unroll
-        for (int v = 0; v < 2; ++v) {
-            const float4 c = *reinterpret_cast<const float4*>(row + at + 4 * v);
-            const float4 s = *reinterpret_cast<const float4*>(row + half + at + 4 * v);
-            const float cc[4] = {c.x, c.y, c.z, c.w}, ss[4] = {s.x, s.y, s.z, s.w};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                t.c[4 * v + i] = cc[i];
-                t.s[4 * v + i] = low ? -ss[i] : ss[i];
-            }
-        }
-    }
-}
-
-// The lane's dims of a row's norm weights (1 without a norm).
-__device__ __forceinline__ void load_weight(const uint16_t* norm, int j, float (&w)[kLaneDims])
-{
-    if (norm != nullptr)
-        unpack8(*reinterpret_cast<const uint4*>(norm + kLaneDims * j), w);
 }
 
 // Norm and rotation of the row that 16 lanes hold.
@@ -266,6 +246,8 @@ __global__ __launch_bounds__(kRopeThreads) void rope_append_token(RopeArgs a)
     const int b = blockIdx.x / a.parts;
     const int at = (int)(blockIdx.x % a.parts) * kRopeRows + threadIdx.x / kRowLanes;
     const int j = threadIdx.x % kRowLanes;
+    if (at >= a.num_q_heads + 2 * a.num_kv_heads)
+        return;
     const int L = a.seq_lens[b];
     int64_t token = b;
     if (a.q_start != nullptr) {
@@ -273,33 +255,29 @@ __global__ __launch_bounds__(kRopeThreads) void rope_append_token(RopeArgs a)
         if (a.q_start[b + 1] <= token)
             return;
     }
-    if (L < 0)
-        return;
-    const bool first = threadIdx.x == 0 && blockIdx.x % a.parts == 0;
-    if (L >= a.max_pages * kPageSize || L >= a.num_positions) {
-        if (first)
-            report(a, RL_DA_DEVERR_LENGTH_TOO_LONG);
-        return;
-    }
-    const int32_t page = a.block_table[(int64_t)b * a.max_pages + L / kPageSize];
-    if (page < 0 || (int64_t)page >= a.num_pages) {
-        if (first)
-            report(a, RL_DA_DEVERR_PAGE_OUT_OF_RANGE);
-        return;
-    }
-    if (at >= a.num_q_heads + 2 * a.num_kv_heads)
-        return;
+    // A token that has no place is left out at the end, and its reads go to position 0: the
+    // row is read beside the length, and the page beside the cosines.
     const HeadRow r = head_row(a, at);
     const uint4 bits = *reinterpret_cast<const uint4*>(row_source(a, r, token) + kLaneDims * j);
-    float x[kLaneDims];
+    const uint16_t* norm = r.is_q ? a.q_norm : (r.is_v ? nullptr : a.k_norm);
+    const uint4 weight = *reinterpret_cast<const uint4*>(
+        norm != nullptr ? norm + kLaneDims * j : row_source(a, r, token) + kLaneDims * j);
+    const bool fits = L < a.max_pages * kPageSize && L < a.num_positions;
+    const int pos = fits ? max(L, 0) : 0;
+    const int32_t page = a.block_table[(int64_t)b * a.max_pages + pos / kPageSize];
+    Turn t;
+    load_turn<INTERLEAVED>(a, pos, j, t);
+    float x[kLaneDims], w[kLaneDims];
     unpack8(bits, x);
-    if (!r.is_v) {
-        Turn t;
-        float w[kLaneDims];
-        load_turn<INTERLEAVED>(a, L, j, t);
-        const uint16_t* norm = r.is_q ? a.q_norm : a.k_norm;
-        load_weight(norm, j, w);
-        turn_row<INTERLEAVED>(a, norm, w, t, j, x);
+    unpack8(weight, w);
+    turn_row<INTERLEAVED>(a, norm, w, t, j, x);
+    if (r.is_v)
+        unpack8(bits, x);
+    const bool in_pool = page >= 0 && (int64_t)page < a.num_pages;
+    if (L < 0 || !fits || !in_pool) {
+        if (L >= 0 && j == 0 && at == 0)
+            report(a, fits ? RL_DA_DEVERR_PAGE_OUT_OF_RANGE : RL_DA_DEVERR_LENGTH_TOO_LONG);
+        return;
     }
     if (r.is_q) {
         *reinterpret_cast<uint4*>(a.q_out + (token * a.num_q_heads + r.head) * kHeadDim +
@@ -370,10 +348,12 @@ __global__ __launch_bounds__(kRopeThreads) void rope_append_pages(RopeArgs a)
     const int held = tile == 0 ? L % kPageSize : 0;  // slots of earlier tokens
     const int64_t row_at = page * a.page_bytes + (int64_t)slot * a.row_bytes;
     Turn t;
-    float wq[kLaneDims], wk[kLaneDims];
     load_turn<INTERLEAVED>(a, live ? pos : 0, j, t);
-    load_weight(a.q_norm, j, wq);
-    load_weight(a.k_norm, j, wk);
+    float wq[kLaneDims] = {}, wk[kLaneDims] = {};
+    if (a.q_norm != nullptr) {
+        unpack8(*reinterpret_cast<const uint4*>(a.q_norm + kLaneDims * j), wq);
+        unpack8(*reinterpret_cast<const uint4*>(a.k_norm + kLaneDims * j), wk);
+    }
 
     // kAhead head rows are read side by side (50k prompt tokens of 48 head rows, bf16 and
     // e4m3: four 245 and 349 us, six 241 and 244, eight 246 and 282; one at a time and
@@ -514,6 +494,8 @@ rl_da_status rl_rope_append(const void* q, int64_t q_stride, const void* k_new, 
     PoolStrides ps;
     if (!pool_strides(layout, num_kv_heads, fp8 ? 1 : 2, &ps))
         return RL_DA_ERR_INVALID_ARG;
+    if (ps.page >= ((int64_t)1 << 31))  // strides inside a page are 32-bit
+        return RL_DA_ERR_UNSUPPORTED;
     if (batch == 0 || max_q_per_seq == 0)
         return RL_DA_OK;
     RopeArgs a;

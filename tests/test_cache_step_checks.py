@@ -50,6 +50,8 @@ def rope(**kw):
     (UNSUPPORTED, dict(rotary_dim=8)), (UNSUPPORTED, dict(rotary_dim=72)),
     (UNSUPPORTED, dict(rotary_dim=144)), (UNSUPPORTED, dict(max_pages=1 << 27)),
     (UNSUPPORTED, dict(batch=1 << 20, max_q_per_seq=1 << 20)),
+    # pages of 2 GiB: 2^19 kv heads in bf16
+    (UNSUPPORTED, dict(num_kv_heads=1 << 19, k_stride=1 << 26, v_stride=1 << 26)),
 ])
 def test_rope_append_host_checks(status, kw):
     assert rope(**kw) == status, kw
@@ -81,6 +83,7 @@ def prefix(**kw):
     (UNSUPPORTED, dict(head_dim=64)), (UNSUPPORTED, dict(page_size=8)),
     (UNSUPPORTED, dict(num_q_heads=24)), (UNSUPPORTED, dict(num_q_heads=256)),
     (UNSUPPORTED, dict(batch=1 << 30)), (UNSUPPORTED, dict(max_pages=1 << 27)),
+    (UNSUPPORTED, dict(num_q_heads=1 << 19, num_kv_heads=1 << 19)),
 ])
 def test_prefix_attn_host_checks(status, kw):
     assert prefix(**kw) == status, kw
