@@ -348,7 +348,8 @@ rl_da_status rl_kv_append(const void* k_new, const void* v_new, void* k_pool, vo
  *                Dims from rotary_dim on are not rotated
  *   q_norm, k_norm  [head_dim] bf16 weights, both or neither
  *   q_out        [T][num_q_heads][head_dim] bf16, T = q_start[batch] (batch); may be
- *                q itself if q_stride is num_q_heads * head_dim
+ *                q itself if q_stride is num_q_heads * head_dim, else apart from the
+ *                inputs
  * bf16 pools: the row rounded to bf16.  e4m3 pools: as rl_kv_append, with all new
  * tokens of a (page, kv head) slab joining at once: scale' = max over the earlier
  * scale (if the slab holds earlier tokens of the sequence) and the new tokens'
@@ -363,8 +364,9 @@ rl_da_status rl_kv_append(const void* k_new, const void* v_new, void* k_pool, vo
  * [0, num_pages) (RL_DA_DEVERR_PAGE_OUT_OF_RANGE): nothing of a skipped token is
  * written, its row of q_out included.  Needs no handle and no workspace; enqueues
  * one kernel on `stream`.  Any rl_da_layout; head_dim 128, page_size 16, rotary_dim
- * a multiple of 16 up to 128, pages (all kv heads) under 2 GiB only (else UNSUPPORTED); q, k_new, v_new, cos_sin, the
- * norm weights, q_out and the pools 16-byte aligned.
+ * a multiple of 16 up to 128, pages (all kv heads) under 2 GiB only (else
+ * UNSUPPORTED); q, k_new, v_new, cos_sin, the norm weights, q_out and the pools
+ * 16-byte aligned.
  */
 rl_da_status rl_rope_append(const void* q, int64_t q_stride, const void* k_new, int64_t k_stride,
                             const void* v_new, int64_t v_stride, const int32_t* q_start,
@@ -393,16 +395,17 @@ rl_da_status rl_rope_append(const void* q, int64_t q_stride, const void* k_new, 
  *                 0 .. max_pages)
  * A sequence of fewer than prefix_pages * page_size tokens is no member of its
  * group: it attends its own row, and may hold anything there if it is empty.  q,
- * pools, scales, block_table, seq_lens and out as for rl_decode_attn_run;
- * num_groups 0 (group_start and prefix_pages then unread) is a plain decode step.
+ * pools, scales, block_table, seq_lens and out as for rl_decode_attn_run, out apart
+ * from q; num_groups 0 (group_start and prefix_pages then unread) is a plain decode
+ * step.
  *
  * The workspace is device memory of at least rl_prefix_attn_workspace_size bytes
  * for these sizes, 16-byte aligned; the launches of this call alone write and read
  * it, so it needs no initial contents, may be reused or freed once the stream has
  * passed them, and calls that can overlap bring one each.  Enqueues one to three
- * kernels on `stream` and allocates nothing.  Deterministic: keys are cut where the call's sizes
- * and the sequence's and its prefix's lengths say, and a row's partial results join
- * in a fixed order.
+ * kernels on `stream` and allocates nothing.  Deterministic: keys are cut where the
+ * call's sizes and the sequence's and its prefix's lengths say, a group's rows are
+ * tiled by their number, and a row's partial results join in a fixed order.
  *
  * Block-table entries are checked on the device: one outside [0, num_pages) among a
  * sequence's (a group's shared) pages is reported in device_error, when that is

@@ -506,6 +506,12 @@ def _device_index(device):
     return torch.cuda.current_device() if device.index is None else device.index
 
 
+def _converted(fn, first, values):
+    """values as the C types of fn's arguments from number `first` on: converted once here
+    instead of on every call."""
+    return tuple(None if v is None else t(v) for t, v in zip(fn.argtypes[first:], values))
+
+
 def _on_device(index, fn, *args):
     """fn(*args) with the GPU `index` current, where the library launches."""
     import torch
@@ -574,13 +580,14 @@ class RopeAppender:
         self._held = (p.k_pool, p.v_pool, p.k_scale, p.v_scale, p.block_table, p.seq_lens,
                       cos_sin, q_norm, k_norm, device_error)
         self._fn = load_library().rl_rope_append
-        self._turn_args = (_ptr(cos_sin), int(cos_sin.shape[0]), int(cos_sin.shape[1]),
-                           int(bool(interleaved)), _ptr(q_norm), _ptr(k_norm), float(eps))
-        self._cache_args = (
+        self._turn_args = _converted(self._fn, 8, (
+            _ptr(cos_sin), int(cos_sin.shape[0]), int(cos_sin.shape[1]),
+            int(bool(interleaved)), _ptr(q_norm), _ptr(k_norm), float(eps)))
+        self._cache_args = _converted(self._fn, 16, (
             _ptr(p.k_pool), _ptr(p.v_pool), _ptr(p.k_scale), _ptr(p.v_scale), int(p.num_pages),
             _ptr(p.block_table), int(p.max_pages), _ptr(p.seq_lens), int(p.batch),
             int(p.num_q_heads), int(p.num_kv_heads), int(p.head_dim), int(p.page_size), dt,
-            LAYOUTS[p.layout], _ptr(device_error))
+            LAYOUTS[p.layout], _ptr(device_error)))
         self._index = _device_index(dev)
 
     def __call__(self, q, k_new, v_new, q_out, q_start=None, max_q_per_seq=1, stream=None):
@@ -680,12 +687,14 @@ class PrefixAttention:
         self._held = (p.k_pool, p.v_pool, p.k_scale, p.v_scale, p.block_table, p.seq_lens,
                       group_start, prefix_pages, device_error)
         self._fn = load_library().rl_prefix_attn
-        self._before = (_ptr(p.k_pool), _ptr(p.v_pool), _ptr(p.k_scale), _ptr(p.v_scale),
-                        int(p.num_pages), _ptr(p.block_table), int(p.max_pages),
-                        _ptr(p.seq_lens), int(p.batch), _ptr(group_start), _ptr(prefix_pages),
-                        groups, int(p.num_q_heads), int(p.num_kv_heads), int(p.head_dim),
-                        int(p.page_size), dt, LAYOUTS[p.layout], float(p.scale))
-        self._behind = (_ptr(workspace), int(workspace.shape[0]), _ptr(device_error))
+        self._before = _converted(self._fn, 1, (
+            _ptr(p.k_pool), _ptr(p.v_pool), _ptr(p.k_scale), _ptr(p.v_scale), int(p.num_pages),
+            _ptr(p.block_table), int(p.max_pages), _ptr(p.seq_lens), int(p.batch),
+            _ptr(group_start), _ptr(prefix_pages), groups, int(p.num_q_heads),
+            int(p.num_kv_heads), int(p.head_dim), int(p.page_size), dt, LAYOUTS[p.layout],
+            float(p.scale)))
+        self._behind = _converted(self._fn, 21, (
+            _ptr(workspace), int(workspace.shape[0]), _ptr(device_error)))
 
     def _own_workspace(self, nbytes):
         """Memory that any stream may use at once: the allocator hands out memory whose

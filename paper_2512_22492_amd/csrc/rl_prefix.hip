@@ -1577,6 +1577,10 @@ rl_da_status rl_prefix_attn(const void* q, const void* k_pool, const void* v_poo
         return RL_DA_ERR_INVALID_ARG;
     if (batch == 0)
         return RL_DA_OK;
+    // a group's rows are read by work-groups that others' outputs do not wait for
+    const uintptr_t row_bytes = (uintptr_t)batch * num_q_heads * kHeadDim * sizeof(uint16_t);
+    if ((uintptr_t)q < (uintptr_t)out + row_bytes && (uintptr_t)out < (uintptr_t)q + row_bytes)
+        return RL_DA_ERR_INVALID_ARG;
     PrefixArgs a;
     a.q = (const uint16_t*)q;
     a.k_pool = (const uint8_t*)k_pool;

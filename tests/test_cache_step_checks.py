@@ -60,7 +60,7 @@ def test_rope_append_host_checks(status, kw):
 def prefix(**kw):
     args = dict(q=FAKE, k_pool=FAKE, v_pool=FAKE, k_scale=None, v_scale=None, num_pages=16,
                 block_table=FAKE, max_pages=4, seq_lens=FAKE, batch=0, group_start=FAKE,
-                prefix_pages=FAKE, num_groups=3, num_q_heads=32, num_kv_heads=8, out=FAKE,
+                prefix_pages=FAKE, num_groups=3, num_q_heads=32, num_kv_heads=8, out=2 * FAKE,
                 workspace=FAKE, workspace_bytes=1 << 40)
     args.update(kw)
     return B.rl_prefix_attn(**args)
@@ -77,9 +77,11 @@ def prefix(**kw):
     (INVALID, dict(num_kv_heads=0)), (INVALID, dict(scale=float("inf"))),
     (INVALID, dict(kv_dtype=2)), (INVALID, dict(kv_dtype=1)),
     (INVALID, dict(k_scale=FAKE, v_scale=FAKE)), (INVALID, dict(layout=-1)),
-    (INVALID, dict(layout=2)), (INVALID, dict(q=FAKE + 8)), (INVALID, dict(out=FAKE + 2)),
+    (INVALID, dict(layout=2)), (INVALID, dict(q=FAKE + 8)), (INVALID, dict(out=2 * FAKE + 2)),
     (INVALID, dict(v_pool=FAKE + 4)), (INVALID, dict(workspace=FAKE + 8)),
     (INVALID, dict(batch=2, workspace_bytes=255)),
+    (INVALID, dict(batch=2, out=FAKE)), (INVALID, dict(batch=2, out=FAKE + 2 * 32 * 256 - 16)),
+    (INVALID, dict(batch=2, out=FAKE - 16)),
     (UNSUPPORTED, dict(head_dim=64)), (UNSUPPORTED, dict(page_size=8)),
     (UNSUPPORTED, dict(num_q_heads=24)), (UNSUPPORTED, dict(num_q_heads=256)),
     (UNSUPPORTED, dict(batch=1 << 30)), (UNSUPPORTED, dict(max_pages=1 << 27)),
