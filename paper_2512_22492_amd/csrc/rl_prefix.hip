@@ -1448,18 +1448,26 @@ constexpr int kResident = 256 * 2;
 
 // How many units a call's shared and own runs are cut into, kv heads included, and the
 // least pages of one.  A call whose (sequence, kv head) pairs leave the device idle is
-// cut finely, into one round of units in all; one that fills it coarsely, since units
-// and their partial results cost more there (8 responses of 1000..8000 tokens to one
-// prompt of 2000, 8 kv heads: 39.5 us cut coarsely, 31.6 finely; 64 responses of 2000 to 8
-// prompts 105.5 coarsely, 114.4 finely).
+// cut finely, into one round of units; one that fills it coarsely, since units and their
+// partial results cost more there (8 responses of 1000..8000 tokens to one prompt of
+// 2000, 8 kv heads: 39.5 us cut coarsely, 31.6 finely; 64 responses of 2000 to 8 prompts
+// 105.5 coarsely, 114.4 finely).  Own runs of a call of a round or two are cut into
+// two rounds and more, so that what is left over is short; everything else into no more
+// than a round, which a few units past it would double (56 pairs of 675 shared pages: ten splits 58 us, nine
+// 44.6; 120 of 499: five splits 110, four 98).
 struct SplitGoal {
     int shared, own, least_shift;
+    bool past_round;
 };
-constexpr SplitGoal kFewPairs = {512, 512, 4}, kManyPairs = {512, 1024, 5};
+constexpr SplitGoal kFewPairs = {512, 512, 4, false}, kManyPairs = {512, 1024, 5, true};
+constexpr int kFew = kResident / 2;  // pairs
 
-int wanted_splits(int64_t target, int64_t pairs)
+int wanted_splits(int64_t target, int64_t pairs, bool past)
 {
-    return (int)((target + pairs - 1) / (pairs > 0 ? pairs : 1));
+    if (pairs < 1)
+        pairs = 1;
+    const int64_t n = (target + (past ? pairs - 1 : 0)) / pairs;
+    return (int)(n > 1 ? n : 1);
 }
 
 // false: sizes past what the kernels index
@@ -1472,13 +1480,13 @@ bool lay_out(int32_t max_pages, int32_t batch, int32_t num_groups, int32_t num_q
         return false;
     const int64_t tiles = (rows + kTileRows - 1) / kTileRows + num_groups;
     const int64_t pairs = (int64_t)batch * num_kv_heads;
-    const SplitGoal& goal = pairs < kResident ? kFewPairs : kManyPairs;
+    const SplitGoal& goal = pairs <= kFew ? kFewPairs : kManyPairs;
     w->least_shift = goal.least_shift;
-    w->wanted_own = wanted_splits(goal.own, pairs);
+    w->wanted_own = wanted_splits(goal.own, pairs, goal.past_round);
     // a group's rows share the splits of its prefix among 128-row tiles at least
     const int64_t shared_pairs =
         (int64_t)num_kv_heads * (num_groups > rows / kTileRows ? num_groups : rows / kTileRows);
-    w->wanted_shared = wanted_splits(goal.shared, shared_pairs);
+    w->wanted_shared = wanted_splits(goal.shared, shared_pairs, false);
     // splits_of takes at most pages / kMaxSplitPages + 1 or `wanted`, whichever is more
     const int32_t least = max_pages / kMaxSplitPages + 1;
     const int32_t most = (max_pages >> goal.least_shift) + 1;

@@ -63,7 +63,7 @@ struct RopeArgs {
     int32_t rotary_dim;
     float norm_eps;
     int32_t parts;              // work-groups that share a sequence's (page's) head rows
-    int32_t tiles;              // pages a sequence's new tokens may touch
+    int32_t tiles;              // a sequence's new tokens, or the pages they may touch
 };
 
 __device__ __forceinline__ void report(const RopeArgs& a, int32_t bits)
@@ -238,20 +238,22 @@ __device__ __forceinline__ const uint16_t* row_source(const RopeArgs& a, const H
     return base + r.head * kHeadDim;
 }
 
-// One token per sequence: 16 head rows per work-group, `parts` work-groups per
-// sequence.
+// One token per sequence, or into bf16 pages, where nothing joins the tokens of a page,
+// a few: 16 head rows of one token per work-group, `parts` work-groups per token and
+// `tiles` tokens per sequence.
 template <bool FP8, bool INTERLEAVED>
 __global__ __launch_bounds__(kRopeThreads) void rope_append_token(RopeArgs a)
 {
-    const int b = blockIdx.x / a.parts;
+    const int step = (int)(blockIdx.x / a.parts) % a.tiles;
+    const int b = (int)(blockIdx.x / a.parts) / a.tiles;
     const int at = (int)(blockIdx.x % a.parts) * kRopeRows + threadIdx.x / kRowLanes;
     const int j = threadIdx.x % kRowLanes;
     if (at >= a.num_q_heads + 2 * a.num_kv_heads)
         return;
-    const int L = a.seq_lens[b];
+    const int before = a.seq_lens[b];
     int64_t token = b;
     if (a.q_start != nullptr) {
-        token = a.q_start[b];
+        token = (int64_t)a.q_start[b] + step;
         if (a.q_start[b + 1] <= token)
             return;
     }
@@ -262,8 +264,9 @@ __global__ __launch_bounds__(kRopeThreads) void rope_append_token(RopeArgs a)
     const uint16_t* norm = r.is_q ? a.q_norm : (r.is_v ? nullptr : a.k_norm);
     const uint4 weight = *reinterpret_cast<const uint4*>(
         norm != nullptr ? norm + kLaneDims * j : row_source(a, r, token) + kLaneDims * j);
+    const int64_t L = before + (int64_t)step;
     const bool fits = L < a.max_pages * kPageSize && L < a.num_positions;
-    const int pos = fits ? max(L, 0) : 0;
+    const int pos = fits && before >= 0 ? (int)L : 0;
     const int32_t page = a.block_table[(int64_t)b * a.max_pages + pos / kPageSize];
     Turn t;
     load_turn<INTERLEAVED>(a, pos, j, t);
@@ -274,8 +277,8 @@ __global__ __launch_bounds__(kRopeThreads) void rope_append_token(RopeArgs a)
     if (r.is_v)
         unpack8(bits, x);
     const bool in_pool = page >= 0 && (int64_t)page < a.num_pages;
-    if (L < 0 || !fits || !in_pool) {
-        if (L >= 0 && j == 0 && at == 0)
+    if (before < 0 || !fits || !in_pool) {
+        if (before >= 0 && j == 0 && at == 0)
             report(a, fits ? RL_DA_DEVERR_PAGE_OUT_OF_RANGE : RL_DA_DEVERR_LENGTH_TOO_LONG);
         return;
     }
@@ -284,7 +287,7 @@ __global__ __launch_bounds__(kRopeThreads) void rope_append_token(RopeArgs a)
                                   kLaneDims * j) = pack8(x);
         return;
     }
-    const int slot = L % kPageSize;
+    const int slot = pos % kPageSize;
     uint8_t* codes = (r.is_v ? a.v_pool : a.k_pool) + page * a.page_bytes +
                      (int64_t)r.head * a.head_bytes;
     if (!FP8) {
@@ -440,6 +443,10 @@ __global__ __launch_bounds__(kRopeThreads) void rope_append_pages(RopeArgs a)
 constexpr int64_t kPageGroups = 4096;
 constexpr int64_t kMinParts = 4;
 
+// Up to so many tokens per sequence into bf16 pages take a work-group each, of which a
+// page's sixteen slots would leave most idle (%FEW%).
+constexpr int32_t kFewTokens = 8;
+
 }  // namespace
 
 extern "C" {
@@ -527,9 +534,9 @@ rl_da_status rl_rope_append(const void* q, int64_t q_stride, const void* k_new, 
     a.num_positions = num_positions;
     a.rotary_dim = rotary_dim;
     a.norm_eps = norm_eps;
-    const bool one = max_q_per_seq == 1;
-    // pages that max_q_per_seq tokens from any slot on touch at most
-    a.tiles = one ? 1 : (int32_t)(((int64_t)max_q_per_seq + 14) / kPageSize + 1);
+    const bool one = max_q_per_seq <= (fp8 ? 1 : kFewTokens);
+    // tokens of a sequence, or the pages that they touch at most from any slot on
+    a.tiles = one ? max_q_per_seq : (int32_t)(((int64_t)max_q_per_seq + 14) / kPageSize + 1);
     const int64_t pages = (int64_t)batch * a.tiles;
     if (one) {
         a.parts = (int32_t)((heads + kRopeRows - 1) / kRopeRows);
