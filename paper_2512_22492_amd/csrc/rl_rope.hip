@@ -30,6 +30,11 @@ constexpr int kRopeThreads = 256;
 constexpr int kRopeRows = kRopeThreads / kRowLanes;  // rows in flight per work-group
 constexpr int kLaneDims = kHeadDim / kRowLanes;
 static_assert(kRopeRows == kPageSize, "a work-group's rows are the slots of a page");
+// Calls of up to so many tokens per sequence go by tokens and head rows instead of pages,
+// most of whose sixteen slots they would leave idle: 512 sequences x 48 head rows of two
+// tokens 38 -> 10.6 us, of eight 43 -> 21, of twelve 45 -> 37, of sixteen 46 -> 49
+// (bf16); e4m3 %FEW8%.
+constexpr int kFewTokens = 8;
 constexpr int kAhead = 6;  // head rows that a thread of rope_append_pages has in flight
 constexpr int kDppRowRor8 = 0x128;
 
@@ -309,6 +314,93 @@ __global__ __launch_bounds__(kRopeThreads) void rope_append_token(RopeArgs a)
         *scale = now;
 }
 
+// A few tokens per sequence into e4m3 pages: sixteen lanes take one head row of all the
+// new tokens of one page that they touch, at most kFewTokens, and hold them until the
+// slab's largest magnitude is known.  The bits are rope_append_pages'.
+template <bool INTERLEAVED>
+__global__ __launch_bounds__(kRopeThreads) void rope_append_few(RopeArgs a)
+{
+    const int part = blockIdx.x % a.parts;
+    const int tile = (int)(blockIdx.x / a.parts) % a.tiles;
+    const int b = (int)(blockIdx.x / a.parts) / a.tiles;
+    const int at = part * kRopeRows + threadIdx.x / kRowLanes;
+    const int j = threadIdx.x % kRowLanes;
+    const int L = a.seq_lens[b];
+    const int64_t token0 = a.q_start[b];
+    const int n = (int)(a.q_start[b + 1] - token0);
+    if (L < 0 || n <= 0)
+        return;
+    const int64_t end = (int64_t)L + n;
+    const int64_t col = L / kPageSize + tile;  // page of the sequence
+    if (col * kPageSize >= end)
+        return;
+    const bool first = threadIdx.x == 0 && part == 0;
+    const int64_t cap = min((int64_t)a.max_pages * kPageSize, (int64_t)a.num_positions);
+    if (first && min(end, (col + 1) * kPageSize) > cap)
+        report(a, RL_DA_DEVERR_LENGTH_TOO_LONG);
+    const int64_t from = max((int64_t)L, col * kPageSize);  // first position in this page
+    if (from >= cap)
+        return;
+    const int32_t page = a.block_table[(int64_t)b * a.max_pages + col];
+    if (page < 0 || (int64_t)page >= a.num_pages) {
+        if (first)
+            report(a, RL_DA_DEVERR_PAGE_OUT_OF_RANGE);
+        return;
+    }
+    if (at >= a.num_q_heads + 2 * a.num_kv_heads)
+        return;
+    const int live = (int)(min(min(end, cap), (col + 1) * kPageSize) - from);
+    const int64_t token = token0 + (from - L);
+    const HeadRow r = head_row(a, at);
+    const uint16_t* norm = r.is_q ? a.q_norm : (r.is_v ? nullptr : a.k_norm);
+    float w[kLaneDims] = {};
+    if (norm != nullptr)
+        unpack8(*reinterpret_cast<const uint4*>(norm + kLaneDims * j), w);
+    uint4 bits[kFewTokens];
+#pragma unroll
+    for (int i = 0; i < kFewTokens; ++i)  // past the last token its row again
+        bits[i] = *reinterpret_cast<const uint4*>(
+            row_source(a, r, token + min(i, live - 1)) + kLaneDims * j);
+    float x[kFewTokens][kLaneDims], m = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kFewTokens; ++i) {
+        if (i >= live)
+            break;
+        unpack8(bits[i], x[i]);
+        if (!r.is_v) {
+            Turn t;
+            load_turn<INTERLEAVED>(a, (int)from + i, j, t);
+            turn_row<INTERLEAVED>(a, norm, w, t, j, x[i]);
+        }
+        if (r.is_q)
+            *reinterpret_cast<uint4*>(a.q_out +
+                                      ((token + i) * a.num_q_heads + r.head) * kHeadDim +
+                                      kLaneDims * j) = pack8(x[i]);
+        m = fmaxf(m, absmax8(x[i]));
+    }
+    if (r.is_q)
+        return;
+    const int held = tile == 0 ? L % kPageSize : 0;  // slots of earlier tokens
+    uint8_t* codes = (r.is_v ? a.v_pool : a.k_pool) + page * a.page_bytes +
+                     (int64_t)r.head * a.head_bytes + 8 * j;
+    float* scale = (r.is_v ? a.v_scale : a.k_scale) + (int64_t)page * a.num_kv_heads + r.head;
+    const float was = *scale;
+    const float now = joined_scale(row16_max(m), held > 0, was);
+    if (now != was) {  // the slab's earlier tokens at the grown scale
+        for (int s = 0; s < held; ++s) {
+            uint2* c = reinterpret_cast<uint2*>(codes + (int64_t)s * a.row_bytes);
+            *c = shrink8(*c, was / now);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < kFewTokens; ++i)
+        if (i < live)
+            *reinterpret_cast<uint2*>(codes + (from % kPageSize + i) * a.row_bytes) =
+                encode8(x[i], now);
+    if (j == 0)
+        *scale = now;
+}
+
 // Several tokens per sequence: a work-group for one page that a sequence's new
 // tokens touch, its 16 rows the page's slots, and a part of the head rows, which
 // it walks one after another: a row's cosines and sines are read once for all of
@@ -443,10 +535,6 @@ __global__ __launch_bounds__(kRopeThreads) void rope_append_pages(RopeArgs a)
 constexpr int64_t kPageGroups = 4096;
 constexpr int64_t kMinParts = 4;
 
-// Up to so many tokens per sequence into bf16 pages take a work-group each, of which a
-// page's sixteen slots would leave most idle (%FEW%).
-constexpr int32_t kFewTokens = 8;
-
 }  // namespace
 
 extern "C" {
@@ -534,11 +622,12 @@ rl_da_status rl_rope_append(const void* q, int64_t q_stride, const void* k_new, 
     a.num_positions = num_positions;
     a.rotary_dim = rotary_dim;
     a.norm_eps = norm_eps;
-    const bool one = max_q_per_seq <= (fp8 ? 1 : kFewTokens);
+    const bool few = max_q_per_seq <= kFewTokens;
+    const bool one = few && (!fp8 || max_q_per_seq == 1);
     // tokens of a sequence, or the pages that they touch at most from any slot on
     a.tiles = one ? max_q_per_seq : (int32_t)(((int64_t)max_q_per_seq + 14) / kPageSize + 1);
     const int64_t pages = (int64_t)batch * a.tiles;
-    if (one) {
+    if (few) {
         a.parts = (int32_t)((heads + kRopeRows - 1) / kRopeRows);
     } else {
         const int64_t most = (heads + kAhead - 1) / kAhead;
@@ -553,7 +642,7 @@ rl_da_status rl_rope_append(const void* q, int64_t q_stride, const void* k_new, 
     void (*kernel)(RopeArgs) = nullptr;
     auto pick = [&](auto fp8_t, auto inter_t) {
         constexpr bool F = decltype(fp8_t)::value, I = decltype(inter_t)::value;
-        kernel = one ? rope_append_token<F, I> : rope_append_pages<F, I>;
+        kernel = one ? rope_append_token<F, I> : (few ? rope_append_few<I> : rope_append_pages<F, I>);
     };
     if (fp8)
         interleaved ? pick(std::true_type{}, std::true_type{})

@@ -205,6 +205,27 @@ ONE = dict(new=[1] * 9, prior=[0, 1, 14, 15, 16, 17, 100, 255, 256])
 MANY = dict(new=[1, 2, 16, 0, 17, 33, 100, 15, 31], prior=[0, 15, 16, 9, 0, 14, 7, 1, 250])
 
 
+# calls of a few tokens per sequence, within a page and over two
+FEW = dict(new=[1, 2, 8, 0, 7, 8, 3, 5], prior=[0, 15, 8, 9, 9, 0, 30, 250])
+
+
+@pytest.mark.parametrize("layout", LAYOUTS)
+@pytest.mark.parametrize("kv", ["bf16", "fp8_e4m3"])
+@pytest.mark.parametrize("interleaved,rotary", [(False, 128), (False, 96), (True, 128)])
+def test_a_few_tokens_have_the_bits_of_many(interleaved, rotary, kv, layout):
+    """Up to eight tokens per sequence against the definition, and bit for bit what a
+    call gives whose bound allows more (which goes by pages)."""
+    outs = []
+    for most in (8, 9):
+        p = problem(**FEW, kv=kv, layout=layout, seed=15)
+        r = call(p, **FEW, norm=rotary == 128, rotary=rotary, interleaved=interleaved, fused=True,
+                 max_new=most)
+        check_call(p, **FEW, **r)
+        outs.append([r["q_out"]] + [t for t in snapshot(p) if t is not None])
+    for a, b in zip(*outs):
+        assert torch.equal(a.contiguous().view(torch.uint8), b.contiguous().view(torch.uint8))
+
+
 @pytest.mark.parametrize("layout", LAYOUTS)
 @pytest.mark.parametrize("kv", ["bf16", "fp8_e4m3"])
 @pytest.mark.parametrize("shape", [ONE, MANY], ids=["one", "many"])
@@ -276,11 +297,11 @@ def test_without_rotation_the_bytes_are_the_appends(kv, layout):
 
 
 @pytest.mark.parametrize("kv", ["bf16", "fp8_e4m3"])
-@pytest.mark.parametrize("many", [False, True])
+@pytest.mark.parametrize("many", [False, True, "few"])
 def test_tokens_that_have_no_place_are_left_out(many, kv):
     """Negative lengths, positions past the table and past the rotation table, pages
     out of range: reported, and nothing of them is written."""
-    new = [4, 5, 20, 3, 2] if many else [1] * 5
+    new = {False: [1] * 5, True: [4, 5, 20, 3, 2], "few": [4, 5, 8, 3, 2]}[many]
     prior = [-1, 30, 12, 40, 3]
     room = [a + max(b, 0) for a, b in zip(new, prior)]
     p = problem(room, [0] * 5, kv=kv, seed=8, max_pages=4)
