@@ -31,10 +31,11 @@ constexpr int kRopeRows = kRopeThreads / kRowLanes;  // rows in flight per work-
 constexpr int kLaneDims = kHeadDim / kRowLanes;
 static_assert(kRopeRows == kPageSize, "a work-group's rows are the slots of a page");
 // Calls of up to so many tokens per sequence go by tokens and head rows instead of pages,
-// most of whose sixteen slots they would leave idle: 512 sequences x 48 head rows of two
-// tokens 38 -> 10.6 us, of eight 43 -> 21, of twelve 45 -> 37, of sixteen 46 -> 49
-// (bf16); e4m3 %FEW8%.
-constexpr int kFewTokens = 8;
+// most of whose sixteen slots they would leave idle.  512 sequences x 48 head rows, us by
+// pages and so: bf16, two tokens 38 and 10.6, eight 43 and 21, twelve 45 and 37, sixteen
+// 46 and 49; e4m3, whose form holds a page's tokens in registers, two 60 and 12, eight
+// 65 and 25.
+constexpr int kFewTokens = 8, kFewTokensBf16 = 12;
 constexpr int kAhead = 6;  // head rows that a thread of rope_append_pages has in flight
 constexpr int kDppRowRor8 = 0x128;
 
@@ -622,7 +623,7 @@ rl_da_status rl_rope_append(const void* q, int64_t q_stride, const void* k_new, 
     a.num_positions = num_positions;
     a.rotary_dim = rotary_dim;
     a.norm_eps = norm_eps;
-    const bool few = max_q_per_seq <= kFewTokens;
+    const bool few = max_q_per_seq <= (fp8 ? kFewTokens : kFewTokensBf16);
     const bool one = few && (!fp8 || max_q_per_seq == 1);
     // tokens of a sequence, or the pages that they touch at most from any slot on
     a.tiles = one ? max_q_per_seq : (int32_t)(((int64_t)max_q_per_seq + 14) / kPageSize + 1);

@@ -216,7 +216,7 @@ def test_a_few_tokens_have_the_bits_of_many(interleaved, rotary, kv, layout):
     """Up to eight tokens per sequence against the definition, and bit for bit what a
     call gives whose bound allows more (which goes by pages)."""
     outs = []
-    for most in (8, 9):
+    for most in (8, 20):
         p = problem(**FEW, kv=kv, layout=layout, seed=15)
         r = call(p, **FEW, norm=rotary == 128, rotary=rotary, interleaved=interleaved, fused=True,
                  max_new=most)
