@@ -346,3 +346,23 @@ def test_replays_equal_the_eager_run(kv):
         check_close(bf16_to_f64(out), ref, "step %d" % step, extra_abs=extra(p, ref))
         p.seq_lens += 11
     del g
+
+
+@pytest.mark.parametrize("layout", ["hnd", "nhd"])
+def test_pages_beyond_4_gib(layout):
+    """Page offsets past 32 bits: the same pages at the end of a 4.3 GiB pool and in a
+    small one give the same bits, split and whole, shared and own."""
+    small = problem([5, 2], [70, 3], [70 * PAGE + 9 * i for i in range(5)] + [50, 61], hq=32,
+                    hkv=8, layout=layout, seed=95, poison=False)
+    want = run(small)
+    n = small.num_pages
+    pages = (9 << 29) // (8 * PAGE * 128 * 2)            # 4.5 GiB
+    shape = (pages,) + tuple(small.k_pool.shape[1:])
+    k, v = (torch.empty(shape, dtype=torch.bfloat16, device=device()) for _ in range(2))
+    k[-n:], v[-n:] = small.k_pool, small.v_pool
+    big = workloads.DecodeProblem(**{**{f: x for f, x in small.__dict__.items()
+                                        if f not in ("group_start", "prefix_pages")},
+                                     "k_pool": k, "v_pool": v,
+                                     "block_table": small.block_table + (pages - n)})
+    big.group_start, big.prefix_pages = small.group_start, small.prefix_pages
+    assert torch.equal(run(big).view(torch.int16), want.view(torch.int16))

@@ -393,3 +393,37 @@ def test_replays_equal_the_eager_call(kv):
         p.seq_lens += 1
         e.seq_lens += 1
     del g
+
+
+@pytest.mark.parametrize("shape", [ONE, MANY, FEW], ids=["one", "many", "few"])
+def test_pages_beyond_4_gib(shape):
+    """Page offsets past 32 bits: the pages at the end of a 4.3 GiB pool receive what those
+    of a small pool receive."""
+    for kv, gib in (("bf16", 9), ("fp8_e4m3", 9)):
+        small = problem(**shape, hq=8, hkv=8, kv=kv, seed=16)
+        n, page_bytes = small.num_pages, small.k_pool[0].numel() * small.k_pool.element_size()
+        pages = (gib << 29) // page_bytes
+        k, v = (torch.empty((pages,) + tuple(small.k_pool.shape[1:]), dtype=small.k_pool.dtype,
+                            device=device()) for _ in range(2))
+        k[-n:], v[-n:] = small.k_pool, small.v_pool
+        more = {}
+        if kv != "bf16":
+            for name in ("k_scale", "v_scale"):
+                s = torch.ones((pages, 8), device=device())
+                s[-n:] = getattr(small, name)
+                more[name] = s
+        big = workloads.DecodeProblem(**{**small.__dict__, "k_pool": k, "v_pool": v,
+                                         "block_table": small.block_table + (pages - n), **more})
+        outs = []
+        for p in (small, big):
+            q, kn, vn = tokens(p, shape["new"], 17)
+            q_out = torch.empty_like(q)
+            start = torch.tensor(np.concatenate([[0], np.cumsum(shape["new"])]),
+                                 dtype=torch.int32, device=device())
+            B.rope_append(p, q, kn, vn, table(400, D), q_out, start, max(shape["new"]))
+            torch.cuda.synchronize()
+            outs.append([q_out] + [t[-n:] for t in (p.k_pool, p.v_pool, p.k_scale, p.v_scale)
+                                   if t is not None])
+        for a, b in zip(*outs):
+            assert torch.equal(a.contiguous().view(torch.uint8), b.contiguous().view(torch.uint8))
+        del big, k, v, more, outs, p
