@@ -30,9 +30,11 @@ namespace {
 
 constexpr int kMaxSplitPages = kWave * kUnitWaves;  // a lane of each wavefront per page
 // Own runs of up to a page per wavefront of a unit are a wavefront's alone: it has no one
-// to wait for, and a work-group takes four (512 sequences x 8 kv heads of one token 36 -> 19 us,
-// of 64 45 -> 38; at 256 tokens the pages of a unit's four wavefronts overlap better).
-constexpr int kAlonePages = kUnitWaves;
+// to wait for, and a work-group takes four (512 sequences x 8 kv heads of one token
+// 36 -> 19 us); where there are wavefronts' worth of them for several rounds, up to
+// sixteen pages (of 1..200 tokens 61 -> 50 us, e4m3 51 -> 35; 64 sequences of 256 tokens,
+// which are not, 20 -> 38).
+constexpr int kAlonePages = kUnitWaves, kAloneManyPages = 16;
 constexpr int kTileRows = 128;        // query rows of a shared unit at most
 constexpr float kNoScore = -3.0e38f;  // running max before the first key
 
@@ -120,6 +122,7 @@ struct PrefixArgs {
     int32_t wanted_shared;      // splits that fill the device (splits_of)
     int32_t wanted_own;
     int32_t least_shift;        // log2 of a split's least pages
+    int32_t alone_pages;        // own runs up to this length are a wavefront's
     float scale_log2;           // |scale| * log2(e)
     uint32_t q_sign;            // 0x80008000 for a negative scale: Q enters negated
 };
@@ -149,7 +152,10 @@ __device__ __forceinline__ Unit scalar_unit(const Unit& u)
 struct Own {
     int len, first, shared;  // tokens, first own page, partial results of the shared ones
     Splits s;
-    __device__ __forceinline__ bool alone() const { return s.count == 1 && s.pages <= kAlonePages; }
+    __device__ __forceinline__ bool alone(const PrefixArgs& a) const
+    {
+        return s.count == 1 && s.pages <= a.alone_pages;
+    }
 };
 __device__ __forceinline__ Own own_of(const PrefixArgs& a, int len, int shared_pages)
 {
@@ -276,7 +282,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_prefix(PrefixArgs a)
         return own_of(a, length_of(b), g >= 0 ? shared_pages(a, pages[g]) : 0);
     };
     auto own_class = [&](const Own& o) {
-        return o.alone() ? kClasses + length_class(o.s.pages * kUnitWaves)
+        return o.alone(a) ? kClasses + length_class(min(o.s.pages * kUnitWaves, kMaxSplitPages))
                          : length_class(o.s.pages);
     };
     auto shared_at = [&](int g) { return shared_of(a, starts[g], starts[g + 1], pages[g]); };
@@ -433,7 +439,7 @@ __device__ __forceinline__ void plan_small(const PrefixArgs& a, SmallPlan& plan,
                         len >= group_pages * kPageSize;
     const Own o = own_of(a, len, member ? group_pages : 0);
     const uint64_t members = __ballot(member);
-    const bool alone = o.alone();
+    const bool alone = o.alone(a);
     const uint64_t alone_mask = __ballot(alone);
     if (alone)
         plan.alone_seq[__popcll(alone_mask & ((1ull << lane) - 1))] = lane;
@@ -1624,6 +1630,8 @@ rl_da_status rl_prefix_attn(const void* q, const void* k_pool, const void* v_poo
     a.wanted_shared = w.wanted_shared;
     a.wanted_own = w.wanted_own;
     a.least_shift = w.least_shift;
+    a.alone_pages = (int64_t)batch * num_kv_heads >= kUnitWaves * kResident ? kAloneManyPages
+                                                                           : kAlonePages;
     a.scale_log2 = fabsf(scale) * kLog2e;
     a.q_sign = scale < 0.0f ? 0x80008000u : 0u;
     hipStream_t st = (hipStream_t)stream;
