@@ -23,6 +23,13 @@ namespace {
 //
 // Three launches: plan_prefix (one work-group) writes the list of units from the
 // lengths and groups on the device, attend_prefix takes them, merge_prefix joins.
+// Calls of few sequences are planned inside attend_prefix, and calls of few rows and a
+// narrow table are one launch of attend_rows, which shares nothing.
+//
+// What bounds it: HBM while a key meets up to some 100 query rows (64 prompts x 8
+// responses, 4600 MB to read: 729 us, 6.3 TB/s), the matrix and vector units above (256
+// sequences x 16 heads under 8192 tokens: 104 us, 0.67 PFLOP/s over the call, 0.97 in its
+// stages), launches and load latency in small calls (9 us).
 //
 // A sequence shorter than its group's prefix is not a member: it attends all its
 // keys as its own.  So every row of a shared unit sees every key of it, and a

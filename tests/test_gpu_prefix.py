@@ -166,13 +166,14 @@ def test_no_groups_is_a_decode_step():
     check_close(bf16_to_f64(out), ref, extra_abs=extra(p, ref))
 
 
-def test_more_sequences_and_groups_than_the_plan_has_threads():
+@pytest.mark.parametrize("groups", [1500, 2500, 5000])
+def test_more_sequences_and_groups_than_the_plan_has_threads(groups):
     rng = np.random.default_rng(6)
-    sizes = [int(x) for x in rng.integers(0, 3, 2500)]
-    prefix = [int(x) for x in rng.integers(0, 3, 2500)]
+    sizes = [int(x) for x in rng.integers(0, 3, groups)]
+    prefix = [int(x) for x in rng.integers(0, 3, groups)]
     lens = np.repeat(prefix, sizes) * PAGE + rng.integers(0, 20, sum(sizes))
     p = problem(sizes, prefix, lens, hq=1, hkv=1, seed=70, poison=False)
-    check(p, "2500 groups")
+    check(p, "%d groups of %d sequences" % (groups, sum(sizes)))
 
 
 @pytest.mark.parametrize("kv", ["bf16", "fp8_e4m3"])
