@@ -41,7 +41,8 @@ def problem(sizes, prefix, lengths, hq=8, hkv=2, kv="bf16", layout="hnd", seed=1
                                layout=layout, max_pages=max(max_pages or 0, width))
     table = p.block_table.clone()
     for g, n in enumerate(prefix):
-        table[start[g]:start[g + 1], :n] = table[start[g], :n].clone()
+        if sizes[g]:
+            table[start[g]:start[g + 1], :n] = table[start[g], :n].clone()
     p.block_table = table
     p.seq_lens = torch.tensor(lengths, dtype=torch.int32)
     if poison:
