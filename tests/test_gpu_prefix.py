@@ -22,7 +22,12 @@ def extra(p, ref):
     weights to one bf16 each, normalised by the sum of the same rounded weights in
     bf16 pools and of the unrounded ones in e4m3 pools: at most P_ROUND (M1 + |o|)
     either way, as worked out for extend."""
+    # A rounding by a relative e changes a sum of w_j c_j s_j by at most e sum w_j |c_j| |s_j|
+    # = e M1.  oracle_ref clears the codes' signs only, so |s_j| is passed in; with the
+    # positive scales of other tests that is the same number.
+    signed, p.v_scale = p.v_scale, None if p.v_scale is None else p.v_scale.abs()
     m1 = oracle_ref(p, abs_values=True)
+    p.v_scale = signed
     return P_ROUND * (m1 + np.abs(ref)) + PV_ROUND * m1
 
 
@@ -368,3 +373,28 @@ def test_pages_beyond_4_gib(layout):
                                      "block_table": small.block_table + (pages - n)})
     big.group_start, big.prefix_pages = small.group_start, small.prefix_pages
     assert torch.equal(run(big).view(torch.int16), want.view(torch.int16))
+
+
+@pytest.mark.parametrize("size", [1, 6, 14, 40])
+def test_page_scales_of_any_sign(size):
+    """e4m3 slabs whose scales are negative or zero, under every way to share a unit (4, 24,
+    56 and 128 query rows), with a call's scale of either sign."""
+    n = size + 60                                  # past what is planned in the kernel
+    p = problem([size], [70], [70 * PAGE + 5 * i for i in range(size)] + [20] * 60, hq=4, hkv=1,
+                kv="fp8_e4m3", seed=96, behind=60)
+    p.k_scale[::3] *= -1.0
+    p.k_scale[1::7] = 0.0
+    p.v_scale[::5] *= -2.0
+    for scale in (p.scale, -2.0 * p.scale):
+        p.scale = scale
+        check(p, "%d of %d, scale %g" % (size, n, scale))
+
+
+@pytest.mark.parametrize("kv", ["bf16", "fp8_e4m3"])
+@pytest.mark.parametrize("size", [6, 14, 40])
+def test_steep_scores_under_shared_units(size, kv):
+    """One key takes nearly all the weight, and another one further on."""
+    p = problem([size] + [1] * 60, [70] + [0] * 60,
+                [70 * PAGE + 5 * i for i in range(size)] + [3] * 60, hq=4, hkv=1, kv=kv, seed=97)
+    p.q.mul_(40.0)
+    check(p, "steep, %d %s" % (size, kv))
