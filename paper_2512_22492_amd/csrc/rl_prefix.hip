@@ -4,6 +4,7 @@
 #include <type_traits>
 
 #include "rl_tile.h"
+#include "rl_turns.h"
 
 using namespace rl_da;
 
@@ -525,7 +526,7 @@ struct AttendLds {
     float2 ml[kUnitWaves][32];
     __attribute__((aligned(16))) int32_t pages[kMaxSplitPages + kStagePages];
     __attribute__((aligned(16))) float2 scales[kMaxSplitPages + kStagePages];
-    int next_unit;
+    NextPlace next;  // of the list, for all wavefronts
 };
 
 struct Lanes {
@@ -1297,7 +1298,7 @@ attend_prefix(PrefixArgs a)
     // than one round, deals them out in turn).
     const int xcd = blockIdx.x % kXcds;
     int at = blockIdx.x;
-    while (at < total) {
+    for (int turn = 0; at < total; ++turn) {
         // made anew for each unit: what a unit derives from them would otherwise be kept
         // in registers throughout, for all four ways
         Lanes lanes;
@@ -1341,9 +1342,11 @@ attend_prefix(PrefixArgs a)
             }
         }
         if (!SMALL && threadIdx.x == 0)
-            lds.next_unit = next_place(a, total, xcd, taken);
+            lds.next.of(turn) = next_place(a, total, xcd, taken);
         __syncthreads();  // the next unit's loads overwrite what this one still read
-        at = SMALL ? at + (int)gridDim.x : __builtin_amdgcn_readfirstlane(lds.next_unit);
+        // (runs of a wavefront alone have no other barrier: what keeps thread 0's next write
+        // from this read is that it goes to the other word)
+        at = SMALL ? at + (int)gridDim.x : __builtin_amdgcn_readfirstlane(lds.next.of(turn));
     }
 }
 
