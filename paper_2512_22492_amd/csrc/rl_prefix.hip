@@ -3,6 +3,7 @@
 
 #include <type_traits>
 
+#include "rl_prefix_rule.h"
 #include "rl_tile.h"
 #include "rl_turns.h"
 
@@ -36,37 +37,10 @@ namespace {
 // keys as its own.  So every row of a shared unit sees every key of it, and a
 // finished sequence (length 0) takes part in nothing.
 
-constexpr int kMaxSplitPages = kWave * kUnitWaves;  // a lane of each wavefront per page
-// Own runs of up to a page per wavefront of a unit are a wavefront's alone: it has no one
-// to wait for, and a work-group takes four (512 sequences x 8 kv heads of one token
-// 36 -> 19 us); where there are wavefronts' worth of them for several rounds, up to
-// sixteen pages (of 1..200 tokens 61 -> 50 us, e4m3 51 -> 35; 64 sequences of 256 tokens,
-// which are not, 20 -> 38).
-constexpr int kAlonePages = kUnitWaves, kAloneManyPages = 16;
-constexpr int kTileRows = 128;        // query rows of a shared unit at most
+static_assert(kMaxSplitPages == kWave * kUnitWaves, "a lane of each wavefront per page");
+static_assert(kAlonePages == kUnitWaves, "a page per wavefront of a unit");
+static_assert(kSmallCall == kWave, "a lane per sequence and per group");
 constexpr float kNoScore = -3.0e38f;  // running max before the first key
-
-// Splits of a run of `pages` pages: no longer than kMaxSplitPages, and as many as
-// `wanted`, what the call's shape needs to fill the device, of 2^least_shift pages at
-// least.  Depends on the run's own length and the call's sizes only.
-struct Splits {
-    int count, pages, more;  // splits; pages of each, and one more of the first `more`
-    __device__ __forceinline__ int first(int i) const { return i * pages + min(i, more); }
-    __device__ __forceinline__ int size(int i) const { return pages + (i < more ? 1 : 0); }
-};
-__device__ __forceinline__ Splits splits_of(int pages, int wanted, int least_shift)
-{
-    Splits s;
-    s.count = max((pages + kMaxSplitPages - 1) / kMaxSplitPages,
-                  min(pages >> least_shift, wanted));
-    s.pages = pages;
-    s.more = 0;
-    if (s.count > 1) {
-        s.pages = pages / s.count;
-        s.more = pages - s.pages * s.count;
-    }
-    return s;
-}
 
 // A unit of work for each kv head: query rows row0 .. row0 + rows - 1 (row = sequence
 // * G + head of the group) against pages page0 .. of a table row.
@@ -395,11 +369,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_prefix(PrefixArgs a)
     }
 }
 
-// The plan of a small call, which every work-group of the attention kernel makes for
-// itself, a lane per sequence and per group: the launch of plan_prefix and the wait for
-// it cost 3 us (four responses to a short prompt 15.2 -> 12.2).
-constexpr int kSmallCall = kWave;  // sequences and groups at most
-
+// The plan of a small call (rl_prefix_rule.h).
 struct SmallPlan {
     // running numbers of units, and what each is made from
     int shared_end[kSmallCall], own_end[kSmallCall];
@@ -1455,36 +1425,8 @@ __global__ __launch_bounds__(kMergeThreads) void merge_prefix(PrefixArgs a)
 
 struct Workspace {
     int64_t leaders, parts, units, ml, acc, bytes;  // offsets
-    int32_t wanted_shared, wanted_own, least_shift, slots;
-    int64_t max_units;
+    PrefixRule rule;
 };
-
-// Work-groups that the device holds at once.
-constexpr int kResident = 256 * 2;
-
-// How many units a call's shared and own runs are cut into, kv heads included, and the
-// least pages of one.  A call whose (sequence, kv head) pairs leave the device idle is
-// cut finely, into one round of units; one that fills it coarsely, since units and their
-// partial results cost more there (8 responses of 1000..8000 tokens to one prompt of
-// 2000, 8 kv heads: 39.5 us cut coarsely, 31.6 finely; 64 responses of 2000 to 8 prompts
-// 105.5 coarsely, 114.4 finely).  Own runs of a call of a round or two are cut into
-// two rounds and more, so that what is left over is short; everything else into no more
-// than a round, which a few units past it would double (56 pairs of 675 shared pages: ten splits 58 us, nine
-// 44.6; 120 of 499: five splits 110, four 98).
-struct SplitGoal {
-    int shared, own, least_shift;
-    bool past_round;
-};
-constexpr SplitGoal kFewPairs = {512, 512, 4, false}, kManyPairs = {512, 1024, 5, true};
-constexpr int kFew = kResident / 2;  // pairs
-
-int wanted_splits(int64_t target, int64_t pairs, bool past)
-{
-    if (pairs < 1)
-        pairs = 1;
-    const int64_t n = (target + (past ? pairs - 1 : 0)) / pairs;
-    return (int)(n > 1 ? n : 1);
-}
 
 // false: sizes past what the kernels index
 bool lay_out(int32_t max_pages, int32_t batch, int32_t num_groups, int32_t num_q_heads,
@@ -1494,51 +1436,20 @@ bool lay_out(int32_t max_pages, int32_t batch, int32_t num_groups, int32_t num_q
     if (rows > INT32_MAX / 2 || (int64_t)batch * num_q_heads > INT32_MAX ||
         (int64_t)max_pages * kPageSize > INT32_MAX - kPageSize)
         return false;
-    const int64_t tiles = (rows + kTileRows - 1) / kTileRows + num_groups;
-    const int64_t pairs = (int64_t)batch * num_kv_heads;
-    const SplitGoal& goal = pairs <= kFew ? kFewPairs : kManyPairs;
-    w->least_shift = goal.least_shift;
-    w->wanted_own = wanted_splits(goal.own, pairs, goal.past_round);
-    // a group's rows share the splits of its prefix among 128-row tiles at least
-    const int64_t shared_pairs =
-        (int64_t)num_kv_heads * (num_groups > rows / kTileRows ? num_groups : rows / kTileRows);
-    w->wanted_shared = wanted_splits(goal.shared, shared_pairs, false);
-    // splits_of takes at most pages / kMaxSplitPages + 1 or `wanted`, whichever is more
-    const int32_t least = max_pages / kMaxSplitPages + 1;
-    const int32_t most = (max_pages >> goal.least_shift) + 1;
-    const int32_t shared = least > (w->wanted_shared < most ? w->wanted_shared : most)
-                               ? least
-                               : (w->wanted_shared < most ? w->wanted_shared : most);
-    const int32_t own = least > (w->wanted_own < most ? w->wanted_own : most)
-                            ? least
-                            : (w->wanted_own < most ? w->wanted_own : most);
-    w->slots = shared + own;
-    w->max_units = tiles * shared + (int64_t)batch * own;
-    if (w->max_units * num_kv_heads > INT32_MAX / 2)
+    const PrefixRule r = prefix_rule(max_pages, batch, num_groups, num_q_heads, num_kv_heads);
+    if (r.max_units * num_kv_heads > INT32_MAX / 2)
         return false;
+    w->rule = r;
     auto round = [](int64_t n) { return (n + 255) / 256 * 256; };
     w->leaders = round((int64_t)sizeof(Queue));
     w->parts = w->leaders + round((int64_t)num_groups * (int64_t)sizeof(int32_t));
     w->units = w->parts + round((int64_t)batch * (int64_t)sizeof(int2));
-    w->ml = w->units + round(w->max_units * (int64_t)sizeof(Unit));
-    const int64_t partials = (int64_t)batch * num_q_heads * w->slots;
+    w->ml = w->units + round(r.max_units * (int64_t)sizeof(Unit));
+    const int64_t partials = (int64_t)batch * num_q_heads * r.slots;
     w->acc = w->ml + round(partials * (int64_t)sizeof(float2));
     w->bytes = w->acc + round(partials * kHeadDim * (int64_t)sizeof(float));
     return true;
 }
-
-// Fewer output rows than this are merged by a work-group each: a call of few rows cuts
-// their keys into many splits, and its merge is bound by walking them.
-constexpr int kSpreadRows = 2048;
-
-// In calls whose (sequence, kv head) pairs fit the device at once a short prefix is read
-// with each sequence's own pages: it comes from the caches, and a unit and a partial
-// result less is worth more (16 responses of up to 80 tokens to 2 prompts of 400, 8 kv heads: 16.7 -> 13.5
-// us; 150 to 600: 19.9 -> 17.1).
-constexpr int kUnsharedPages = 48;
-// Tables up to this width are then attended row by row altogether (the same
-// calls with tables as wide as they need: 16.6 -> 9.0 us, 19.8 -> 11.8; 64 pages 23.0 -> 14.8).
-constexpr int kRowPages = 64;
 
 }  // namespace
 
@@ -1634,18 +1545,17 @@ rl_da_status rl_prefix_attn(const void* q, const void* k_pool, const void* v_poo
     a.num_kv_heads = num_kv_heads;
     a.group_shift = __builtin_ctz((unsigned)G);
     a.max_pages = max_pages;
-    a.max_units = (int32_t)w.max_units;
-    a.slots = w.slots;
-    a.unshared_pages = (int64_t)batch * num_kv_heads <= kResident ? kUnsharedPages : 0;
-    a.wanted_shared = w.wanted_shared;
-    a.wanted_own = w.wanted_own;
-    a.least_shift = w.least_shift;
-    a.alone_pages = (int64_t)batch * num_kv_heads >= kUnitWaves * kResident ? kAloneManyPages
-                                                                           : kAlonePages;
+    a.max_units = (int32_t)w.rule.max_units;
+    a.slots = w.rule.slots;
+    a.unshared_pages = w.rule.unshared_pages;
+    a.wanted_shared = w.rule.wanted_shared;
+    a.wanted_own = w.rule.wanted_own;
+    a.least_shift = w.rule.least_shift;
+    a.alone_pages = w.rule.alone_pages;
     a.scale_log2 = fabsf(scale) * kLog2e;
     a.q_sign = scale < 0.0f ? 0x80008000u : 0u;
     hipStream_t st = (hipStream_t)stream;
-    if (max_pages <= kRowPages && (int64_t)batch * num_kv_heads <= kResident) {
+    if (w.rule.by_rows) {
         const dim3 grid((unsigned)(batch * num_kv_heads));
         if (fp8)
             hipLaunchKernelGGL(attend_rows<true>, grid, dim3(kAttendThreads), 0, st, a);
@@ -1653,7 +1563,7 @@ rl_da_status rl_prefix_attn(const void* q, const void* k_pool, const void* v_poo
             hipLaunchKernelGGL(attend_rows<false>, grid, dim3(kAttendThreads), 0, st, a);
         return hipGetLastError() == hipSuccess ? RL_DA_OK : RL_DA_ERR_HIP;
     }
-    const bool small = batch <= kSmallCall && num_groups <= kSmallCall;
+    const bool small = w.rule.small;
     if (!small) {
         if (batch <= kPlanSequences && num_groups <= kPlanGroups)
             hipLaunchKernelGGL(plan_prefix<true>, dim3(1), dim3(kPlanThreads), 0, st, a);
@@ -1662,7 +1572,7 @@ rl_da_status rl_prefix_attn(const void* q, const void* k_pool, const void* v_poo
         if (hipGetLastError() != hipSuccess)
             return RL_DA_ERR_HIP;
     }
-    const int64_t most = w.max_units * num_kv_heads;
+    const int64_t most = w.rule.max_units * num_kv_heads;
     const dim3 grid((unsigned)(most < kResident ? (most + kXcds - 1) / kXcds * kXcds : kResident));
     void (*attend)(PrefixArgs) = fp8 ? (small ? attend_prefix<true, true> : attend_prefix<true, false>)
                                      : (small ? attend_prefix<false, true>
