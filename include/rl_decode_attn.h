@@ -387,6 +387,13 @@ rl_da_status rl_rope_append(const void* q, int64_t q_stride, const void* k_new, 
  * with each group's shared pages read once instead of once per sequence (short
  * prefixes of calls that leave the device idle may be read with each sequence's own
  * pages, which is faster there).
+ *
+ * Softmax weights enter the value product as in rl_decode_attn_run, in two bf16 terms
+ * (2^-16 of a weight), but for the shared keys of groups of more than 64 query rows per
+ * kv head (n sequences x num_q_heads / num_kv_heads), in e4m3 pools more than 32: there
+ * a weight may be one bf16 term, as in rl_extend_attn, and an output off by 2^-8 of
+ * (weighted mean of |v|) + |output| beside its own rounding (measured: 2.3e-3 of the
+ * outputs' norm against 64 bits instead of 1.7e-3, most of either that rounding).
  *   group_start   [num_groups + 1] int32, non-decreasing: group g is sequences
  *                 group_start[g] .. group_start[g + 1] - 1; sequences before the first
  *                 group and behind the last share nothing

@@ -477,10 +477,14 @@ __device__ __forceinline__ Unit small_unit(const PrefixArgs& a, const SmallPlan&
 //   up to 64, 128 rows (attend_together): 64 keys at a time pass through a double
 //     buffer of the work-group's, one barrier each; a wavefront holds 32 rows and
 //     takes all 64 keys (four wavefronts for 128 rows) or half of them (two pairs for
-//     64 rows, whose halves are joined at the end).  A key read from HBM meets 128
-//     rows, about where the matrix and vector units become the bound, so a weight
-//     enters as one bf16 term.  bf16 pools sum the same rounded weights for the
-//     normaliser, through the value product against ones.
+//     64 rows, whose halves are joined at the end).  Where a byte of keys and values
+//     meets 128 operations, 128 rows of bf16 and 64 of e4m3, the matrix and vector
+//     units are about the bound, and a weight enters as one bf16 term (two: 256 sequences x
+//     16 heads under 8192 tokens 104.4 -> 125.3 us, 64 groups of 64 rows under
+//     1000..4000 e4m3 tokens 124.7 -> 132.8); 64 rows of bf16 take two terms (64 groups
+//     under 2048 tokens 100.2 us with one, 101.3 with two).  bf16 pools sum the same
+//     rounded weights for the normaliser, through the value product against ones, e4m3
+//     pools the unrounded ones: their page's value scale is in the rounded ones.
 
 constexpr int kAttendThreads = kWave * kUnitWaves;
 constexpr int kBuffers = 2;
@@ -878,6 +882,7 @@ __device__ __forceinline__ void attend_together(const PrefixArgs& a, const Unit&
 {
     constexpr int RB = 2;
     constexpr int KB = kStagePages / KW;  // 16-key blocks of a stage per wavefront
+    constexpr int kTerms = KW == 2 && !FP8 ? 2 : 1;  // of a weight
     const int wave = at.wave, lane = at.lane, i16 = at.i16, g4 = at.g4;
     const int kw = wave % KW, row_base = wave / KW * 32;
     const int stages = (u.pages + kStagePages - 1) / kStagePages;
@@ -1094,7 +1099,7 @@ __device__ __forceinline__ void attend_together(const PrefixArgs& a, const Unit&
         }
         // Weights as operands: two 16-key blocks (a half) are one, keys 4 g4 .. + 3 of
         // each.  Piece i of half kh: row block i / 4, key block i / 2 % 2, key pair i % 2.
-        uint32_t pt[RB][KB / 2][4];
+        uint32_t pt[kTerms][RB][KB / 2][4];
         auto make_piece = [&](int kh, int i) {
             const int rb = i / 4, kb = 2 * kh + i / 2 % 2, e = 2 * (i % 2);
             float p0 = exp2_fast(fmaf(s[rb][kb][e], mult[kb], -m[rb]));
@@ -1104,11 +1109,14 @@ __device__ __forceinline__ void attend_together(const PrefixArgs& a, const Unit&
                 p0 *= vs[kb];
                 p1 *= vs[kb];
             }
-            pt[rb][kh][i % 4] = pack_bf16x2(p0, p1);
+            const uint32_t hi = pack_bf16x2(p0, p1);
+            pt[0][rb][kh][i % 4] = hi;
+            if (kTerms == 2)
+                pt[kTerms - 1][rb][kh][i % 4] = pack_bf16x2(p0 - bf16_lo(hi), p1 - bf16_hi(hi));
         };
-        auto operand = [&](int rb, int kh) {
-            return __builtin_bit_cast(bf16x8_t, make_uint4(pt[rb][kh][0], pt[rb][kh][1],
-                                                           pt[rb][kh][2], pt[rb][kh][3]));
+        auto operand = [&](int term, int rb, int kh) {
+            const uint32_t(&w)[4] = pt[term][rb][kh];
+            return __builtin_bit_cast(bf16x8_t, make_uint4(w[0], w[1], w[2], w[3]));
         };
 #pragma unroll
         for (int i = 0; i < 4 * RB; ++i)
@@ -1131,9 +1139,11 @@ __device__ __forceinline__ void attend_together(const PrefixArgs& a, const Unit&
                 next = values(step + 1);
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int rb = 0; rb < RB; ++rb)
-                o[rb][step % 8] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                    v, operand(rb, step / 8), o[rb][step % 8], 0, 0, 0);
+            for (int term = 0; term < kTerms; ++term)
+#pragma unroll
+                for (int rb = 0; rb < RB; ++rb)
+                    o[rb][step % 8] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                        v, operand(term, rb, step / 8), o[rb][step % 8], 0, 0, 0);
             if (KB == 4 && step < 8)
                 make_piece(KB / 2 - 1, step);
         }
@@ -1141,9 +1151,12 @@ __device__ __forceinline__ void attend_together(const PrefixArgs& a, const Unit&
 #pragma unroll
             for (int kh = 0; kh < KB / 2; ++kh)
 #pragma unroll
-                for (int rb = 0; rb < RB; ++rb)
-                    lacc[rb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                        __builtin_bit_cast(bf16x8_t, ones), operand(rb, kh), lacc[rb], 0, 0, 0);
+                for (int term = 0; term < kTerms; ++term)
+#pragma unroll
+                    for (int rb = 0; rb < RB; ++rb)
+                        lacc[rb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                            __builtin_bit_cast(bf16x8_t, ones), operand(term, rb, kh), lacc[rb],
+                            0, 0, 0);
         }
         __builtin_amdgcn_s_setprio(0);
     };

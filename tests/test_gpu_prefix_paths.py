@@ -5,6 +5,7 @@ import pytest
 import torch
 
 from gpu_util import PV_ROUND, bf16_to_f64, check_close, oracle_ref
+from prefix_paths import ways_of
 from test_gpu_prefix import problem, run
 
 pytestmark = pytest.mark.gpu
@@ -36,3 +37,28 @@ def test_work_groups_that_take_short_runs_again_and_again(kv, layout):
     first = check_two_terms(p, "short runs %s %s" % (kv, layout))
     for _ in range(5):
         assert torch.equal(run(p).view(torch.int16), first.view(torch.int16))
+
+
+def grouped(size, pages, own, *, planned=False, before=0, wide=True, **kw):
+    """One group of `size` sequences that share `pages` pages and have own[i % len(own)]
+    tokens of their own; `planned`: among more sequences than a small call has, of one to
+    four tokens."""
+    behind = max(0, 66 - size - before) if planned else 0
+    lens = [3] * before + [pages * PAGE + own[i % len(own)] for i in range(size)] \
+        + [1 + i % 4 for i in range(behind)]
+    return problem([size], [pages], lens, before=before, behind=behind,
+                   max_pages=max(pages + 8, 66) if wide else None, **kw)
+
+
+@pytest.mark.parametrize("planned", [False, True], ids=["small", "planned"])
+@pytest.mark.parametrize("size,hq,way", [(3, 8, "shared16"), (4, 8, "shared16"), (5, 8, "shared32"),
+                                         (8, 8, "shared32"), (9, 8, "shared64"),
+                                         (13, 8, "shared64"), (16, 8, "shared64"),
+                                         (5, 16, "shared64"), (21, 4, "shared64")])
+@pytest.mark.parametrize("pages", [49, 52, 70])
+def test_bf16_groups_of_up_to_64_rows_hold_weights_in_two_terms(pages, size, hq, way, planned):
+    """A weight held in one bf16 term is off by up to 2^-9 of itself, and a sum of some
+    hundred of them by more than what is allowed here."""
+    p = grouped(size, pages, (0, 5, 40, 90), planned=planned, hq=hq, hkv=2, seed=101)
+    assert ways_of(p) >= {way, "planned" if planned else "small"}
+    check_two_terms(p, "%d x %d heads, %d pages" % (size, hq, pages))
