@@ -175,7 +175,8 @@ __device__ __forceinline__ float absmax8(const float (&x)[kLaneDims])
 // "Computation of elementary functions on the IBM RISC System/6000 processor", IBM J.
 // Res. Dev. 34, 1990), three operations an element, as long as nothing leaves the
 // normal range: kScaleLow <= d <= kScaleHigh keeps every a that an e4m3 code tells
-// from zero, and its remainder, far inside it.
+// from zero, and its remainder, far inside it.  What it loses is the sign of a zero (-0 r
+// + 0 is +0) and of a NaN, which the division keeps, and so does a copy of a's sign.
 constexpr float kScaleLow = 0x1p-60f, kScaleHigh = 0x1p60f;
 
 // A row at its slab's scale.  The scale is at least absmax / 448 rounded, so that an
@@ -189,7 +190,7 @@ __device__ __forceinline__ uint2 encode8(const float (&x)[kLaneDims], float scal
 #pragma unroll
         for (int i = 0; i < kLaneDims; ++i) {
             const float q = x[i] * r;
-            y[i] = fmaf(fmaf(-q, scale, x[i]), r, q);
+            y[i] = copysignf(fmaf(fmaf(-q, scale, x[i]), r, q), x[i]);
         }
     } else {
 #pragma unroll
