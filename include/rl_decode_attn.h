@@ -364,9 +364,10 @@ rl_da_status rl_kv_append(const void* k_new, const void* v_new, void* k_pool, vo
  * [0, num_pages) (RL_DA_DEVERR_PAGE_OUT_OF_RANGE): nothing of a skipped token is
  * written, its row of q_out included.  Needs no handle and no workspace; enqueues
  * one kernel on `stream`.  Any rl_da_layout; head_dim 128, page_size 16, rotary_dim
- * a multiple of 16 up to 128, pages (all kv heads) under 2 GiB only (else
- * UNSUPPORTED); q, k_new, v_new, cos_sin, the norm weights, q_out and the pools
- * 16-byte aligned.
+ * a multiple of 16 up to 128, pages (all kv heads) under 2 GiB, launches under 2^24
+ * work-groups only (else UNSUPPORTED; four for each page that a sequence's max_q_per_seq
+ * tokens may touch, or one for 16 head rows of each token where those are few); q,
+ * k_new, v_new, cos_sin, the norm weights, q_out and the pools 16-byte aligned.
  */
 rl_da_status rl_rope_append(const void* q, int64_t q_stride, const void* k_new, int64_t k_stride,
                             const void* v_new, int64_t v_stride, const int32_t* q_start,
@@ -420,7 +421,8 @@ rl_da_status rl_rope_append(const void* q, int64_t q_stride, const void* k_new, 
  * (that group's members) are then undefined; a length beyond max_pages * page_size
  * is cut there and reported with RL_DA_DEVERR_LENGTH_TOO_LONG.  The bits are only
  * ever set.  head_dim 128, page_size 16, Hq / Hkv in {1, 2, 4, 8, 16}, pages (all kv
- * heads) under 2 GiB (else UNSUPPORTED); q, the pools and out 16-byte aligned.
+ * heads) under 2 GiB, batch * num_q_heads under 2^27 - 8 (else UNSUPPORTED); q, the pools
+ * and out 16-byte aligned.
  */
 rl_da_status rl_prefix_attn_workspace_size(int32_t max_pages, int32_t batch, int32_t num_groups,
                                            int32_t num_q_heads, int32_t num_kv_heads,

@@ -1445,12 +1445,12 @@ struct Workspace {
 bool lay_out(int32_t max_pages, int32_t batch, int32_t num_groups, int32_t num_q_heads,
              int32_t num_kv_heads, Workspace* w)
 {
-    const int64_t rows = (int64_t)batch * (num_q_heads / num_kv_heads);  // per kv head
-    if (rows > INT32_MAX / 2 || (int64_t)batch * num_q_heads > INT32_MAX ||
+    // a launch holds fewer than 2^32 threads, and the merge takes 32 for each row
+    if ((int64_t)batch * num_q_heads > UINT32_MAX / 32 - kMergeTeams ||
         (int64_t)max_pages * kPageSize > INT32_MAX - kPageSize)
         return false;
     const PrefixRule r = prefix_rule(max_pages, batch, num_groups, num_q_heads, num_kv_heads);
-    if (r.max_units * num_kv_heads > INT32_MAX / 2)
+    if (r.max_units > INT32_MAX / 2 / num_kv_heads)
         return false;
     w->rule = r;
     auto round = [](int64_t n) { return (n + 255) / 256 * 256; };

@@ -638,7 +638,8 @@ rl_da_status rl_rope_append(const void* q, int64_t q_stride, const void* k_new, 
         if (a.parts > most)
             a.parts = (int32_t)most;
     }
-    if (pages * a.parts > INT32_MAX)
+    // a launch holds fewer than 2^32 threads (pages < 2^31 x 2^27, parts < 2^22)
+    if (pages > UINT32_MAX / kRopeThreads / a.parts)
         return RL_DA_ERR_UNSUPPORTED;
     const dim3 grid((unsigned)(pages * a.parts)), block(kRopeThreads);
     void (*kernel)(RopeArgs) = nullptr;
