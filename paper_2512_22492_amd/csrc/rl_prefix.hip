@@ -37,23 +37,11 @@ namespace {
 // keys as its own.  So every row of a shared unit sees every key of it, and a
 // finished sequence (length 0) takes part in nothing.
 
+static_assert(kRulePage == kPageSize, "one page size");
 static_assert(kMaxSplitPages == kWave * kUnitWaves, "a lane of each wavefront per page");
 static_assert(kAlonePages == kUnitWaves, "a page per wavefront of a unit");
 static_assert(kSmallCall == kWave, "a lane per sequence and per group");
 constexpr float kNoScore = -3.0e38f;  // running max before the first key
-
-// A unit of work for each kv head: query rows row0 .. row0 + rows - 1 (row = sequence
-// * G + head of the group) against pages page0 .. of a table row.
-struct Unit {
-    int32_t table_row;
-    int32_t page0;
-    int32_t pages;
-    int32_t limit;  // keys of the table row from here on are masked
-    int32_t row0;
-    int32_t rows;   // negated: other units read the same pages
-    int32_t slot;   // partial result's place in the row's list; -1: the row's only one
-    int32_t need;   // rows of sequences shorter than this are left out
-};
 
 // What the plan hands to the attention kernel.  Work-group g runs on XCD g % 8 and takes
 // the work at places p = g mod 8 of the list, so each XCD has a counter in a cache line
@@ -130,79 +118,6 @@ __device__ __forceinline__ Unit scalar_unit(const Unit& u)
             s(u.row0),      s(u.rows),  s(u.slot),  s(u.need)};
 }
 
-// A sequence's own run and its splits.
-struct Own {
-    int len, first, shared;  // tokens, first own page, partial results of the shared ones
-    Splits s;
-    __device__ __forceinline__ bool alone(const PrefixArgs& a) const
-    {
-        return s.count == 1 && s.pages <= a.alone_pages;
-    }
-};
-__device__ __forceinline__ Own own_of(const PrefixArgs& a, int len, int shared_pages)
-{
-    Own o;
-    o.len = len;
-    o.first = shared_pages;
-    o.shared = splits_of(o.first, a.wanted_shared, a.least_shift).count;
-    o.s = splits_of(max((o.len + kPageSize - 1) / kPageSize - o.first, 0), a.wanted_own,
-                    a.least_shift);
-    return o;
-}
-__device__ __forceinline__ Unit own_unit(const PrefixArgs& a, int b, const Own& o, int i)
-{
-    Unit u;
-    u.table_row = b;
-    u.page0 = o.first + o.s.first(i);
-    u.pages = o.s.size(i);
-    u.limit = o.len;
-    u.row0 = b << a.group_shift;
-    u.rows = 1 << a.group_shift;
-    u.slot = o.shared + o.s.count == 1 ? -1 : o.shared + i;
-    u.need = 0;
-    return u;
-}
-
-// A group's shared run: its splits, each for every tile of query rows.
-struct Shared {
-    int s0, rows, tiles, pages;
-    Splits s;
-    __device__ __forceinline__ int units() const { return s.count * tiles; }
-};
-__device__ __forceinline__ int shared_pages(const PrefixArgs& a, int pages)
-{
-    const int p = max(0, min(pages, a.max_pages));
-    return p > a.unshared_pages ? p : 0;
-}
-__device__ __forceinline__ Shared shared_of(const PrefixArgs& a, int start, int end, int pages)
-{
-    Shared h;
-    h.s0 = max(0, min(start, a.batch));
-    h.rows = (max(h.s0, min(end, a.batch)) - h.s0) << a.group_shift;
-    h.tiles = (h.rows + kTileRows - 1) / kTileRows;
-    h.pages = shared_pages(a, pages);
-    h.s = splits_of(h.pages, a.wanted_shared, a.least_shift);
-    return h;
-}
-// Unit i of a group; a split's tiles follow each other: they read the same pages, from
-// the table row of `leader`, a member.
-__device__ __forceinline__ Unit shared_unit(const PrefixArgs& a, const Shared& h, int leader, int i)
-{
-    const int split = i / h.tiles, tile = i % h.tiles;
-    Unit u;
-    u.table_row = leader;
-    u.page0 = h.s.first(split);
-    u.pages = h.s.size(split);
-    u.limit = h.pages * kPageSize;
-    u.row0 = (h.s0 << a.group_shift) + tile * kTileRows;
-    u.rows = min(kTileRows, h.rows - tile * kTileRows);
-    if (h.tiles > 1)
-        u.rows = -u.rows;
-    u.slot = split;
-    u.need = h.pages * kPageSize;
-    return u;
-}
-
 // Writes the units, longest first, and each sequence's number of partial results.
 // Units of one class stand in any order: where a unit's results go does not depend
 // on it.  One work-group, bound by the latency of what it reads: lengths and groups
@@ -244,8 +159,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_prefix(PrefixArgs a)
         atomicOr(a.dev_error, RL_DA_DEVERR_LENGTH_TOO_LONG);
     __syncthreads();
     auto length_of = [&](int b) { return max(0, min(lens[b], cap)); };
-    // The group that a sequence is a member of (it fills the group's shared pages),
-    // or -1.
+    // The group that a sequence is a member of (it fills the group's prefix), or -1.
     auto group_of = [&](int b, int len) {
         int lo = -1, hi = a.num_groups;  // the last group that starts at or before b
         while (hi - lo > 1) {
@@ -257,11 +171,12 @@ __global__ __launch_bounds__(kPlanThreads) void plan_prefix(PrefixArgs a)
         }
         if (lo < 0 || starts[lo + 1] <= b)
             return -1;
-        const int p = shared_pages(a, pages[lo]);
+        const int p = prefix_of(a, pages[lo]);
         return p > 0 && len >= p * kPageSize ? lo : -1;
     };
     auto own_at = [&](int b, int g) {
-        return own_of(a, length_of(b), g >= 0 ? shared_pages(a, pages[g]) : 0);
+        return own_of(a, length_of(b), g >= 0 ? prefix_of(a, pages[g]) : 0,
+                      g >= 0 && starts[g + 1] - starts[g] > 1);
     };
     auto own_class = [&](const Own& o) {
         return o.alone(a) ? kClasses + length_class(min(o.s.pages * kUnitWaves, kMaxSplitPages))
@@ -340,7 +255,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_prefix(PrefixArgs a)
         for (uint64_t more = __ballot(o.s.count > kFirst); more != 0; more &= more - 1) {
             const int from = __builtin_ctzll(more);
             auto of = [&](int v) { return __builtin_amdgcn_readlane(v, from); };
-            const Own w = {of(o.len), of(o.first), of(o.shared),
+            const Own w = {of(o.len), of(o.first), of(o.shared), of(o.others),
                            {of(o.s.count), of(o.s.pages), of(o.s.more)}};
             for (int i = kFirst + lane; i < w.s.count; i += kWave)
                 put(of(at) + i, own_unit(a, b0 + from, w, i));
@@ -399,7 +314,7 @@ __device__ __forceinline__ void plan_small(const PrefixArgs& a, SmallPlan& plan,
     const int raw = is_seq ? a.seq_lens[lane] : 0;
     const int start = is_group ? a.group_start[lane] : INT32_MAX;
     const int end = is_group ? a.group_start[lane + 1] : INT32_MAX;
-    const int pages = is_group ? shared_pages(a, a.prefix_pages[lane]) : 0;
+    const int pages = is_group ? prefix_of(a, a.prefix_pages[lane]) : 0;
     const int len = max(0, min(raw, cap));
     // the last group that starts at or before the lane's sequence
     int lo = -1, hi = a.num_groups;
@@ -412,10 +327,11 @@ __device__ __forceinline__ void plan_small(const PrefixArgs& a, SmallPlan& plan,
             hi = below ? hi : mid;
         }
     }
-    const int group_end = __shfl(end, max(lo, 0)), group_pages = __shfl(pages, max(lo, 0));
+    const int group_start = __shfl(start, max(lo, 0)), group_end = __shfl(end, max(lo, 0));
+    const int group_pages = __shfl(pages, max(lo, 0));
     const bool member = is_seq && lo >= 0 && group_end > lane && group_pages > 0 &&
                         len >= group_pages * kPageSize;
-    const Own o = own_of(a, len, member ? group_pages : 0);
+    const Own o = own_of(a, len, member ? group_pages : 0, group_end - group_start > 1);
     const uint64_t members = __ballot(member);
     const bool alone = o.alone(a);
     const uint64_t alone_mask = __ballot(alone);
@@ -523,8 +439,11 @@ __device__ __forceinline__ uint32_t lds_address(const void* p)
 }
 
 // dma16, with the non-temporal hint for bytes that no other unit reads: they would
-// only push others' out of the caches (64 prompts x 8 responses: 806 us without it,
-// 736 with; 1024 e4m3 sequences of 512..2048 tokens 498, 452).
+// only push others' out of the caches (64 prompts x 8 responses of 32 query heads to 8 kv
+// heads: 806 us without it, 736 with; 1024 e4m3 sequences of 512..2048 tokens, the same
+// heads, 498, 452).  A prefix that each member reads with its own pages goes without it
+// (32 groups of 4 sequences of 4 kv heads under 48 pages 33.7 -> 28.6 us, 32 of 8 of 2
+// kv heads 35.6 -> 29.1; 64 of 8 kv heads under 16 pages 14.6 -> 15.5).
 __device__ __forceinline__ void bring16(const uint8_t* gaddr, uint32_t lds, bool once)
 {
     if (once)
@@ -848,11 +767,11 @@ __device__ __forceinline__ void attend_apart(const PrefixArgs& a, const Unit& u,
 // A whole short own run by one wavefront.
 template <bool FP8>
 __device__ __forceinline__ void attend_alone(const PrefixArgs& a, const Unit& u, int kvh,
-                                             AttendLds& lds, const Lanes& at)
+                                             bool once, AttendLds& lds, const Lanes& at)
 {
     float m[1], l[1];
     floatx4_t o[1][8];
-    walk_pages<1, 1, FP8>(a, u, kvh, 0, true, lds, at, m, l, o);
+    walk_pages<1, 1, FP8>(a, u, kvh, 0, once, lds, at, m, l, o);
     const float sum = sum_lanes_xor32(sum_lanes_xor16(l[0]));
     if (at.i16 >= u.rows)
         return;
@@ -1321,7 +1240,9 @@ attend_prefix(PrefixArgs a)
                 } else {
                     u = a.units[planned + n];
                 }
-                attend_alone<FP8>(a, u, item % a.num_kv_heads, lds, lanes);
+                const bool once = u.rows > 0;
+                u.rows = once ? u.rows : -u.rows;
+                attend_alone<FP8>(a, u, item % a.num_kv_heads, once, lds, lanes);
             }
         }
         if (!SMALL && threadIdx.x == 0)

@@ -32,6 +32,39 @@ void part(int pages, int wanted, int least_shift, int i, int* out)
     const Splits s = splits_of(pages, wanted, least_shift);
     out[0] = s.first(i), out[1] = s.size(i);
 }
+struct Call : PrefixRule { int batch, max_pages, group_shift; };
+// A sequence's units as the plans make them, eight numbers each; returns their number.
+// group: the sequence's, as far as it is a member (-1: of none).
+static int put(const Unit& u, int* out)
+{
+    const int v[] = {u.table_row, u.page0, u.pages, u.limit, u.row0, u.rows, u.slot, u.need};
+    for (int i = 0; i < 8; ++i)
+        out[i] = v[i];
+    return 8;
+}
+int own_units(int max_pages, int batch, int groups, int hq, int hkv, int b, int len, int prefix,
+              int company, int* parts, int* out)
+{
+    Call a;
+    static_cast<PrefixRule&>(a) = prefix_rule(max_pages, batch, groups, hq, hkv);
+    a.batch = batch, a.max_pages = max_pages, a.group_shift = __builtin_ctz(hq / hkv);
+    const Own o = own_of(a, len, prefix, company);
+    parts[0] = o.shared, parts[1] = o.s.count;
+    for (int i = 0; i < o.s.count; ++i)
+        out += put(own_unit(a, b, o, i), out);
+    return o.s.count;
+}
+int shared_units(int max_pages, int batch, int groups, int hq, int hkv, int start, int end,
+                 int prefix, int leader, int* out)
+{
+    Call a;
+    static_cast<PrefixRule&>(a) = prefix_rule(max_pages, batch, groups, hq, hkv);
+    a.batch = batch, a.max_pages = max_pages, a.group_shift = __builtin_ctz(hq / hkv);
+    const Shared h = shared_of(a, start, end, prefix);
+    for (int i = 0; i < h.units(); ++i)
+        out += put(shared_unit(a, h, leader, i), out);
+    return h.units();
+}
 int tile_rows() { return kTileRows; }
 int resident() { return kResident; }
 int most_pages() { return kMaxSplitPages; }
@@ -66,6 +99,37 @@ def splits(pages, wanted, least_shift):
     out = (ctypes.c_int * 3)()
     library().splits(pages, wanted, least_shift, out)
     return tuple(out)
+
+
+UNIT = ("table_row", "page0", "pages", "limit", "row0", "rows", "slot", "need")
+
+
+def units(max_pages, hq, hkv, lengths, group_start, prefix_pages):
+    """(the units of a call that is not attended by rows, each a dict; every sequence's
+    numbers of shared and own partial results)."""
+    lib, batch, groups = library(), len(lengths), len(prefix_pages)
+    sizes = (max_pages, batch, groups, hq, hkv)
+    buf, n = (ctypes.c_int * (8 * 4096))(), (ctypes.c_int * 2)()
+    found, parts = [], []
+
+    def take(count):
+        for i in range(count):
+            found.append(dict(zip(UNIT, buf[8 * i:8 * i + 8])))
+
+    member = {}
+    for g in range(groups):
+        inside = [b for b in range(group_start[g], group_start[g + 1])
+                  if prefix_pages[g] and lengths[b] >= prefix_pages[g] * PAGE]
+        member.update({b: g for b in inside})
+        if inside:
+            take(lib.shared_units(*sizes, group_start[g], group_start[g + 1], prefix_pages[g],
+                                  inside[0], buf))
+    for b, length in enumerate(lengths):
+        g = member.get(b)
+        take(lib.own_units(*sizes, b, length, 0 if g is None else prefix_pages[g],
+                           g is not None and group_start[g + 1] - group_start[g] > 1, n, buf))
+        parts.append(tuple(n))
+    return found, parts
 
 
 def ways(max_pages, hq, hkv, lengths, group_start, prefix_pages):
