@@ -559,7 +559,7 @@ rl_da_status rl_rope_append(const void* q, int64_t q_stride, const void* k_new, 
     if (batch < 0 || max_q_per_seq < 0 || num_q_heads <= 0 || num_kv_heads <= 0 ||
         max_pages < 1 || num_pages < 1 || num_positions < 1 || rotary_dim < 1)
         return RL_DA_ERR_INVALID_ARG;
-    if (q_start == nullptr && max_q_per_seq > 1)
+    if (q_start == nullptr && max_q_per_seq != 1)
         return RL_DA_ERR_INVALID_ARG;
     if ((q_norm != nullptr) != (k_norm != nullptr) ||
         (q_norm != nullptr && !(isfinite(norm_eps) && norm_eps >= 0.0f)))

@@ -1,9 +1,11 @@
-"""The largest calls of rl_rope_append and rl_prefix_attn: what no launch can hold is
-answered UNSUPPORTED on the host, before anything reaches a device (CPU)."""
+"""The largest and the smallest calls of rl_rope_append and rl_prefix_attn: what no launch
+can hold is answered UNSUPPORTED on the host, before anything reaches a device, and what
+holds nothing does nothing (CPU)."""
 import pytest
+import torch
 
 from paper_2512_22492_amd import binding as B
-from test_cache_step_checks import prefix, rope
+from test_cache_step_checks import cache, prefix, rope
 
 UNSUPPORTED = B.RL_DA_ERR_UNSUPPORTED
 
@@ -33,3 +35,10 @@ def test_attention_of_more_rows_than_a_merge_launch_holds():
     # units for all kv heads, whose number leaves 64 bits if multiplied out
     assert size(1, 1 << 26, 1 << 26, (1 << 27) - 2, (1 << 31) - 1) == UNSUPPORTED
     assert size(1, 1 << 20, 1 << 20, 1 << 26, (1 << 31) - 1) == UNSUPPORTED
+
+
+def test_one_token_per_sequence_is_a_bound_of_one():
+    """Without q_start every sequence brings a token: a bound of none would drop them."""
+    assert rope(batch=3, q_start=None, max_q_per_seq=0) == B.RL_DA_ERR_INVALID_ARG
+    assert rope(batch=0, q_start=None, max_q_per_seq=0) == B.RL_DA_ERR_INVALID_ARG
+    assert rope(batch=3, max_q_per_seq=0) == B.RL_DA_OK
