@@ -608,7 +608,7 @@ class RopeAppender:
         vs = _token_stride("v_new", v_new, kv_shape, bf16, dev)
         if _token_stride("q_out", q_out, q_shape, bf16, dev) != q_rows[0] * q_rows[1]:
             raise ValueError("q_out must be contiguous")
-        if tokens == 0:
+        if tokens == 0 or self.batch == 0:
             return
         rc = _on_device(self._index, self._fn, q.data_ptr(), qs, k_new.data_ptr(), ks,
                         v_new.data_ptr(), vs, _ptr(q_start), max_q_per_seq, *self._turn_args,
@@ -727,6 +727,8 @@ class PrefixAttention:
         import torch
         _check_tensor("q", q, dtype=torch.bfloat16, shape=self.want, device=self.device)
         _check_tensor("out", out, dtype=torch.bfloat16, shape=self.want, device=self.device)
+        if self.want[0] == 0:
+            return
         if self._streams is not None:
             self._note_stream(stream)
         rc = _on_device(self._index, self._fn, q.data_ptr(), *self._before, out.data_ptr(),

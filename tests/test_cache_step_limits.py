@@ -42,3 +42,21 @@ def test_one_token_per_sequence_is_a_bound_of_one():
     assert rope(batch=3, q_start=None, max_q_per_seq=0) == B.RL_DA_ERR_INVALID_ARG
     assert rope(batch=0, q_start=None, max_q_per_seq=0) == B.RL_DA_ERR_INVALID_ARG
     assert rope(batch=3, max_q_per_seq=0) == B.RL_DA_OK
+
+
+def test_empty_batches_are_no_calls(monkeypatch):
+    """Tensors without elements have no address, which the C entry refuses; a step of no
+    sequences is not an error."""
+    monkeypatch.setattr(B, "_device_index", lambda d: 0)
+    monkeypatch.setattr(B, "_on_device", lambda i, fn, *args: fn(*args))
+    p = cache(batch=0)
+    for groups in (0, 2):
+        attend = B.PrefixAttention(p, torch.zeros(groups + 1, dtype=torch.int32),
+                                   torch.ones(groups, dtype=torch.int32),
+                                   torch.zeros(1 << 16, dtype=torch.uint8))
+        attend(p.q, torch.empty_like(p.q))
+    append = B.RopeAppender(p, torch.zeros((32, 128)))
+    rows = [torch.zeros((5, h, 128), dtype=torch.bfloat16) for h in (4, 2, 2)]
+    append(*(r[:0] for r in rows), rows[0][:0])
+    # rows behind the last sequence's, here all of them, are left as they are
+    append(*rows, torch.ones_like(rows[0]), torch.zeros(1, dtype=torch.int32), 3)
