@@ -387,14 +387,7 @@ rl_da_status rl_rope_append(const void* q, int64_t q_stride, const void* k_new, 
  * 8 of each in the paper's rollouts, Sec. 7.1; a system prompt under all of them),
  * with each group's shared pages read once instead of once per sequence (short
  * prefixes of calls that leave the device idle may be read with each sequence's own
- * pages, which is faster there).
- *
- * Softmax weights enter the value product as in rl_decode_attn_run, in two bf16 terms
- * (2^-16 of a weight), but for the shared keys of groups of more than 64 query rows per
- * kv head (n sequences x num_q_heads / num_kv_heads), in e4m3 pools more than 32: there
- * a weight may be one bf16 term, as in rl_extend_attn, and an output off by 2^-8 of
- * (weighted mean of |v|) + |output| beside its own rounding (measured: 2.3e-3 of the
- * outputs' norm against 64 bits instead of 1.7e-3, most of either that rounding).
+ * pages, for a launch and partial results less).
  *   group_start   [num_groups + 1] int32, non-decreasing: group g is sequences
  *                 group_start[g] .. group_start[g + 1] - 1; sequences before the first
  *                 group and behind the last share nothing
@@ -407,10 +400,18 @@ rl_da_status rl_rope_append(const void* q, int64_t q_stride, const void* k_new, 
  * from q; num_groups 0 (group_start and prefix_pages then unread) is a plain decode
  * step.
  *
+ * Softmax weights enter the value product as in rl_decode_attn_run, in two bf16 terms
+ * (2^-16 of a weight), but for the shared keys of groups of more than 64 query rows per
+ * kv head (n sequences x num_q_heads / num_kv_heads), in e4m3 pools more than 32: there
+ * a weight may be one bf16 term, as in rl_extend_attn, and an output off by 2^-8 of
+ * (weighted mean of |v|) + |output| beside its own rounding (measured: 2.3e-3 of the
+ * outputs' norm against 64 bits instead of 1.7e-3, most of either that rounding).
+ *
  * The workspace is device memory of at least rl_prefix_attn_workspace_size bytes
  * for these sizes, 16-byte aligned; the launches of this call alone write and read
  * it, so it needs no initial contents, may be reused or freed once the stream has
- * passed them, and calls that can overlap bring one each.  Enqueues one to three
+ * passed them, and calls that can overlap bring one each (a captured call's belongs to
+ * its graph for as long as that is replayed).  Enqueues one to three
  * kernels on `stream` and allocates nothing.  Deterministic: keys are cut where the
  * call's sizes and the sequence's and its prefix's lengths say, a group's rows are
  * tiled by their number, and a row's partial results join in a fixed order.

@@ -654,7 +654,8 @@ class PrefixAttention:
 
     workspace: a contiguous uint8 tensor of at least rl_prefix_attn_workspace_size
     bytes for these sizes, by default one of the object's own.  One launch uses it at
-    a time: streams, and captured graphs that can overlap, bring one each."""
+    a time: streams, and captured graphs that can overlap, bring one each.  A graph
+    that captured a call replays it on this workspace: keep the object as long."""
 
     def __init__(self, p, group_start, prefix_pages, workspace=None, device_error=None):
         import torch
@@ -740,7 +741,8 @@ class PrefixAttention:
 def prefix_attention(p, group_start, prefix_pages, out, stream=None, workspace=None,
                      device_error=None):
     """One decode step of problem p (its q) whose groups of sequences share their first
-    pages, as PrefixAttention; raises on a bad status."""
+    pages, as PrefixAttention; raises on a bad status.  To be captured, bring a workspace
+    that the graph's owner keeps, or capture on the current stream."""
     PrefixAttention(p, group_start, prefix_pages, workspace, device_error)(p.q, out, stream)
 
 
