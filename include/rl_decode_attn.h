@@ -331,8 +331,8 @@ rl_da_status rl_kv_append(const void* k_new, const void* v_new, void* k_pool, vo
  *     x <- x / sqrt(mean(x^2) + norm_eps) * w       (w: q_norm or k_norm)
  *     (a, b) <- (a c - b s, b c + a s)              for each pair of x
  * Values are appended as they are.  The arithmetic is fp32, the sum of squares
- * included: a normalised row's elements lie under 2^60, and the mean of their squares
- * plus norm_eps is no denormal number.
+ * included: rows to be normalised hold elements under 2^60, and the mean of their
+ * squares plus norm_eps is no denormal number.
  *   q, k_new, v_new  bf16, head rows [num_q_heads or num_kv_heads][head_dim]
  *                contiguous within a token, tokens q_stride, k_stride, v_stride
  *                elements apart (multiples of 8), so that the three may be views
